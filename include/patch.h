@@ -429,6 +429,106 @@ const char* patch_strerror(patch_status s);
 int patch_last_hip_error(void); /* hipError_t of the most recent PATCH_ERR_HIP on this thread */
 const char* patch_version(void);
 
+/* ---- The attention side of a decoder layer: between the q / k / v product and the output product -----------------
+ *
+ * A paged cache holds the keys and values of many sequences in pages of `page_size` tokens; a row of a page table says which
+ * pages a sequence's tokens are in, in order.  patch_kv_append writes a batch's new tokens into it, patch_attention lets them
+ * attend to everything in it.  All calls are asynchronous on `stream`, allocate nothing, never synchronise, can be captured
+ * into a graph, and give the same bits every time.
+ */
+
+/* Rows of heads side by side: head h of token t begins at element t * stride + h * head_dim. */
+typedef struct {
+    const void* x;       /* DEVICE, fp32 or bf16 (f32), 16-byte aligned; for instance a part of one product's rows               */
+    int64_t stride;      /* elements from one token to the next; a multiple of 16 bytes, at least heads * head_dim               */
+    int heads;
+    int f32;             /* 1: fp32 values, 0: bf16                                                                              */
+    const float* gamma;  /* DEVICE, head_dim factors, 16-byte aligned: each head becomes x / sqrt(mean(x^2) + eps) * gamma (before */
+                         /* the rotation); NULL: no norm                                                                         */
+    void* out;           /* DEVICE, bf16, 16-byte aligned, where the call writes such rows; may be x itself where that is bf16   */
+    int64_t out_stride;  /* its elements from one token to the next, a multiple of 8                                             */
+} patch_heads;
+
+/* Rotation by position: pair i of a head (values i and i + rot_dim / 2, or 2 i and 2 i + 1 if interleaved) is turned by the
+ * angle whose cosine and sine are table[pos][0][i] and table[pos][1][i].  The table is the caller's, so that any scaling of the
+ * frequencies can be in it; computed in 64 bits and rounded once it is good at any position.  Values from rot_dim on stay.
+ * A position at or beyond n_pos turns by NaN. */
+typedef struct {
+    const float* table;  /* DEVICE, n_pos x 2 x rot_dim / 2, 16-byte aligned                                                     */
+    int64_t n_pos;
+    int rot_dim;         /* a multiple of 8, 8 .. head_dim                                                                       */
+    int interleaved;
+    float eps;           /* of the norms                                                                                         */
+} patch_rope;
+
+/* The cache of one layer.  A page holds, for every key head in turn, page_size x head_dim cells of K (token-major) in `k`, and
+ * head_dim x page_size cells of V (feature-major: a feature's tokens side by side) in `v`.  Cells are bf16, or e4m3 (8-bit floats
+ * with 4 exponent bits and no infinities; out of range becomes +-448) of the value over the scale of its head. */
+typedef struct {
+    void* k;                 /* DEVICE, 16-byte aligned                                                                          */
+    void* v;                 /* DEVICE, 16-byte aligned                                                                          */
+    int64_t n_pages;         /* up to 2^31 - 1                                                                                   */
+    int64_t page_stride;     /* cells from one page to the next, in k and in v, a multiple of 16; 0: pages lie side by side      */
+    int page_size;           /* tokens: 16, 32, 64, 128 or 256                                                                   */
+    int kv_heads, head_dim;  /* head_dim: 64, 128 or 256                                                                         */
+    int e4m3;                /* 1: e4m3 cells, 0: bf16                                                                           */
+    const float* k_scale;    /* DEVICE, kv_heads factors (e4m3 only), or NULL: 1                                                 */
+    const float* v_scale;
+} patch_kv_cache;
+
+/* A batch: sequence s has the tokens q_start[s] .. q_start[s + 1] - 1 of the call's rows, the last of its kv_len[s] tokens in
+ * the cache.  So the i-th of its n has position kv_len[s] - n + i.  Sequences of no tokens, or with nothing in the cache, are
+ * fine.  A token whose position is negative has no place: it is not appended, and attends to nothing.
+ * The numbers on the device are not read by the host.  Page numbers outside 0 .. n_pages - 1, and lengths beyond max_kv or
+ * the table, are not followed: patch_kv_append writes nothing there, and the rows of patch_attention that need them are NaN. */
+typedef struct {
+    int64_t n_seqs;             /* 1 .. 65535                                                                                    */
+    int64_t n_tokens;           /* rows of the call: up to 2^23, and up to 2^25 heads of them in patch_attention                 */
+    const int32_t* q_start;     /* DEVICE, n_seqs + 1, never falling; NULL: one token each (n_tokens == n_seqs)                  */
+    const int32_t* kv_len;      /* DEVICE, n_seqs: with the new tokens                                                           */
+    const int32_t* page_table;  /* DEVICE, n_seqs x table_stride: page p of a sequence holds its tokens from p * page_size       */
+    int64_t table_stride;
+    int64_t max_q;              /* no sequence has more tokens in the call (any more get no result); n_tokens would always do    */
+    int64_t max_kv;             /* no kv_len is larger; launches are sized by both, so that close bounds are faster              */
+} patch_seqs;
+
+/* Norm and rotation of Q's and K's heads in one pass: q->out and k->out from q->x and k->x (k may be NULL).
+ *   positions  DEVICE, n_tokens (up to 2^23); a negative one marks a row of padding, which becomes zeros
+ *   rope       NULL: no rotation (and eps = 1e-6)
+ * fp32 inside, rounded to bf16 once.  Errors: PATCH_ERR_ARG, PATCH_ERR_SHAPE (head_dim, rot_dim, strides), PATCH_ERR_HIP. */
+patch_status patch_qk_rope(const patch_heads* q, const patch_heads* k, const int32_t* positions, int64_t n_tokens, int head_dim,
+                           const patch_rope* rope, void* stream);
+
+/* The new tokens of a batch into the cache: K (normed and rotated by its position if asked for) and V (as it is; v->gamma must
+ * be NULL), k->out and v->out unused.  With q (or NULL) also Q, normed and rotated, to q->out for patch_attention, in the same
+ * launch.  rope: NULL = no rotation (and eps = 1e-6).  Where two tokens of a batch have the same cell, either's value is in it.
+ * Errors as patch_qk_rope. */
+patch_status patch_kv_append(const patch_heads* k, const patch_heads* v, const patch_heads* q, const patch_seqs* seqs, const patch_rope* rope,
+                             const patch_kv_cache* cache, void* stream);
+
+typedef struct {
+    float scale;             /* of q . k; 0: 1 / sqrt(head_dim)                                                                  */
+    int64_t prefix_len;      /* the first so many tokens of every sequence of the batch are the same ones: they are read from the */
+                             /* first sequence's row of the page table, once for all rows.  Any number, also inside a page (each */
+                             /* sequence then has its own copy of that page for what follows); 0: nothing shared                 */
+    float* lse;              /* DEVICE out, n_tokens x heads: the logarithm of the sum of exp(score) over a row's keys; or NULL  */
+    void* workspace;         /* DEVICE, 16-byte aligned scratch of the call, or NULL: then nothing is computed once for all and  */
+    size_t workspace_bytes;  /* a sequence's keys are not split over workgroups, which is slower for few rows                    */
+} patch_attention_opts;
+
+/* O[t, h] = sum_j softmax_j(scale q[t, h] . k[j, h / (heads / kv_heads)]) v[j, ...] over the keys j at or before the token's
+ * position in its sequence.
+ *   Q  DEVICE, bf16, n_tokens rows of heads x head_dim, q_stride elements apart (a multiple of 8); heads a multiple of kv_heads
+ *   O  DEVICE, bf16, the same with o_stride; Q itself may be O
+ * A row with no keys becomes zeros (lse: minus infinity).  Rows of tokens that no sequence has are left as they are.
+ * Scores and sums are fp32; a probability is rounded to bf16 before it multiplies V, the result once at the end.
+ * Cells of pages that hold no token yet may hold anything.
+ * Errors: PATCH_ERR_ARG, PATCH_ERR_SHAPE, PATCH_ERR_HIP. */
+patch_status patch_attention(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache* cache, void* O, int64_t o_stride,
+                             void* stream, const patch_attention_opts* opts);
+/* The scratch with which that call splits its keys as finely as it would like (of opts only prefix_len is looked at); 0 for arguments that it refuses. */
+size_t patch_attention_workspace_bytes(int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const patch_attention_opts* opts);
+
 #ifdef __cplusplus
 }
 #endif

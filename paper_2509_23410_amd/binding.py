@@ -25,6 +25,7 @@ EXPORTS = [
     "patch_canonical_sizes", "patch_export_canonical", "patch_packed_bytes", "patch_table_bytes", "patch_packed_dims",
     "patch_packed_tile_map", "patch_packed_row_order", "patch_probe_matrix_rate", "patch_probe_stream_read", "patch_probe_lds_fill", "patch_probe_store_tiles", "patch_probe_lds_read", "patch_gemm4_ex",
     "patch_serialized_bytes", "patch_serialize", "patch_deserialize", "patch_serialized4_bytes", "patch_serialize4", "patch_deserialize4", "patch_free", "patch_strerror", "patch_last_hip_error", "patch_version",
+    "patch_qk_rope", "patch_kv_append", "patch_attention", "patch_attention_workspace_bytes",
 ]
 
 
@@ -41,6 +42,30 @@ class TuneEntry(ctypes.Structure):
     _fields_ = [("m_bucket", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("n_sparse_tiles", ctypes.c_int64),
                 ("tile", ctypes.c_int), ("path", ctypes.c_int), ("split_k", ctypes.c_int), ("variant", ctypes.c_int),
                 ("y_bf16", ctypes.c_int), ("uses_workspace", ctypes.c_int)]
+
+
+class _HeadsC(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("stride", ctypes.c_int64), ("heads", ctypes.c_int), ("f32", ctypes.c_int), ("gamma", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64)]
+
+
+class _RopeC(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("n_pos", ctypes.c_int64), ("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class _KVCacheC(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("page_size", ctypes.c_int),
+                ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("e4m3", ctypes.c_int), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class _SeqsC(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int64), ("n_tokens", ctypes.c_int64), ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("max_q", ctypes.c_int64), ("max_kv", ctypes.c_int64)]
+
+
+class AttentionOpts(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("prefix_len", ctypes.c_int64), ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
 
 
 class PatchError(RuntimeError):
@@ -144,7 +169,13 @@ def lib() -> ctypes.CDLL:
         L.patch_strerror.restype = ctypes.c_char_p
         L.patch_last_hip_error.restype = ci
         L.patch_version.restype = ctypes.c_char_p
-        for f in ("patch_apply_mask", "patch_pack", "patch_gemm", "patch_gemm_ex", "patch_gemm_many", "patch_unpack", "patch_canonical_sizes",
+        pH, pR, pC, pS, pA = (ctypes.POINTER(t) for t in (_HeadsC, _RopeC, _KVCacheC, _SeqsC, AttentionOpts))
+        L.patch_qk_rope.argtypes = [pH, pH, vp, i64, ci, pR, vp]
+        L.patch_kv_append.argtypes = [pH, pH, pH, pS, pR, pC, vp]
+        L.patch_attention.argtypes = [vp, i64, ci, pS, pC, vp, i64, vp, pA]
+        L.patch_attention_workspace_bytes.argtypes = [ci, pS, pC, pA]
+        L.patch_attention_workspace_bytes.restype = sz
+        for f in ("patch_qk_rope", "patch_kv_append", "patch_attention", "patch_apply_mask", "patch_pack", "patch_gemm", "patch_gemm_ex", "patch_gemm_many", "patch_unpack", "patch_canonical_sizes",
                   "patch_export_canonical", "patch_packed_dims", "patch_packed_tile_map", "patch_packed_row_order"):
             getattr(L, f).restype = ci
         _lib = L
@@ -547,3 +578,68 @@ def patch_export_canonical(P: Packed):
     meta = np.zeros(max(mb.value, 1), np.uint8)
     _check(lib().patch_export_canonical(P.handle, vals.ctypes.data, vb.value, meta.ctypes.data, mb.value), "patch_export_canonical")
     return vals, meta[:mb.value]
+
+
+class _Described:
+    """A C descriptor of device buffers (`.c`), which it keeps alive.  Made once and passed to any number of calls."""
+
+    def __init__(self, c, *buffers):
+        self.c, self.ref, self.buffers = c, ctypes.byref(c), buffers
+
+
+class Heads(_Described):
+    """Rows of heads side by side, `stride` elements from one token to the next; see patch_heads in patch.h.  gamma: the heads are
+    normed; out: where the call writes such rows (bf16), out_stride elements apart."""
+
+    def __init__(self, x, heads: int, stride: int, f32: bool = False, gamma=None, out=None, out_stride: int = 0):
+        super().__init__(_HeadsC(_ptr(x), stride, heads, 1 if f32 else 0, _ptr(gamma), _ptr(out), out_stride), x, gamma, out)
+
+
+class Rope(_Described):
+    """Rotation by position: table is n_pos x 2 x rot_dim / 2 fp32, cosines and sines; see patch_rope in patch.h."""
+
+    def __init__(self, table, n_pos: int, rot_dim: int, interleaved: bool = False, eps: float = 1e-6):
+        super().__init__(_RopeC(_ptr(table), n_pos, rot_dim, 1 if interleaved else 0, eps), table)
+
+
+class KVCache(_Described):
+    """The paged keys and values of one layer: k is n_pages x kv_heads x page_size x head_dim, v is n_pages x kv_heads x head_dim x
+    page_size, bf16 or (e4m3) 8-bit cells with a scale per head; see patch_kv_cache in patch.h."""
+
+    def __init__(self, k, v, n_pages: int, page_size: int, kv_heads: int, head_dim: int, e4m3: bool = False, k_scale=None, v_scale=None, page_stride: int = 0):
+        super().__init__(_KVCacheC(_ptr(k), _ptr(v), n_pages, page_stride, page_size, kv_heads, head_dim, 1 if e4m3 else 0, _ptr(k_scale), _ptr(v_scale)),
+                         k, v, k_scale, v_scale)
+
+
+class Seqs(_Described):
+    """A batch of sequences (device int32 kv_len, page_table and q_start); see patch_seqs in patch.h."""
+
+    def __init__(self, n_seqs: int, n_tokens: int, kv_len, page_table, table_stride: int, max_q: int, max_kv: int, q_start=None):
+        super().__init__(_SeqsC(n_seqs, n_tokens, _ptr(q_start), _ptr(kv_len), _ptr(page_table), table_stride, max_q, max_kv), kv_len, page_table, q_start)
+
+
+def patch_qk_rope(q: Heads, k, positions, n_tokens: int, head_dim: int, rope, stream: int = 0) -> None:
+    """q.out, k.out = the heads of q.x, k.x normed (where gamma is given) and rotated (rope given) by device int32 positions; k may be None."""
+    _check(lib().patch_qk_rope(q.ref, k.ref if k else None, _ptr(positions), n_tokens, head_dim, rope.ref if rope else None, stream), "patch_qk_rope")
+
+
+def patch_kv_append(k: Heads, v: Heads, seqs: Seqs, cache: KVCache, stream: int = 0, rope=None, q=None) -> None:
+    """The batch's new K (normed, rotated) and V into its pages; q.out = Q normed and rotated, where q is given."""
+    _check(lib().patch_kv_append(k.ref, v.ref, q.ref if q else None, seqs.ref, rope.ref if rope else None, cache.ref, stream), "patch_kv_append")
+
+
+def patch_attention(Q, heads: int, seqs: Seqs, cache: KVCache, O, stream: int = 0, scale: float = 0.0, prefix_len: int = 0, lse=None, workspace=None,
+                    workspace_bytes=None, q_stride: int = 0, o_stride: int = 0) -> None:
+    """O = causal attention of the batch's rows of Q over its pages, the first prefix_len tokens of every sequence read once for all.  Strides in
+    elements (0: rows side by side).  workspace: a device tensor (or pointer + workspace_bytes) of the call's own; see patch.h."""
+    if workspace is not None and workspace_bytes is None:
+        workspace_bytes = workspace.numel() * workspace.element_size()
+    width = heads * cache.c.head_dim
+    o = AttentionOpts(scale, prefix_len, _ptr(lse), _ptr(workspace), workspace_bytes or 0)
+    _check(lib().patch_attention(_ptr(Q), q_stride or width, heads, seqs.ref, cache.ref, _ptr(O), o_stride or width, stream, ctypes.byref(o)),
+           "patch_attention")
+
+
+def patch_attention_workspace_bytes(heads: int, seqs: Seqs, cache: KVCache, prefix_len: int = 0) -> int:
+    o = AttentionOpts(0.0, prefix_len, None, None, 0)
+    return int(lib().patch_attention_workspace_bytes(heads, seqs.ref, cache.ref, ctypes.byref(o)))

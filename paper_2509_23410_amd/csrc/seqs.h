@@ -1,0 +1,54 @@
+// Device side of a batch of sequences: which tokens a sequence has, where they are in its cache, and page numbers that are checked before use.
+#pragma once
+#include "attention.h"
+#include "epilogue.h"
+
+namespace patch {
+
+template <typename T>
+__device__ __forceinline__ const PATCH_EP_GLOBAL T* as_global(const T* p) {
+    return reinterpret_cast<const PATCH_EP_GLOBAL T*>(reinterpret_cast<uintptr_t>(p));
+}
+template <typename T>
+__device__ __forceinline__ PATCH_EP_GLOBAL T* as_global_out(T* p) {
+    return reinterpret_cast<PATCH_EP_GLOBAL T*>(reinterpret_cast<uintptr_t>(p));
+}
+
+struct Seq {
+    int first, n;    // its tokens in the batch, inside [0, n_tokens] whatever q_start holds
+    int len;         // its tokens in the cache, inside [0, max_kv]
+    int pos0;        // position of its first token in the batch: may be negative, that token then has no place
+    bool bad;        // kv_len beyond what the caller said or the table holds
+};
+
+__host__ __device__ inline int within(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+// from what the device arrays say, whatever that is
+__host__ __device__ inline Seq seq_from(int t0, int t1, int len, int n_tokens, int max_kv) {
+    Seq q;
+    q.first = within(t0, 0, n_tokens);
+    q.n = within(t1, q.first, n_tokens) - q.first;
+    q.bad = len > max_kv;
+    q.len = within(len, 0, max_kv);
+    q.pos0 = q.len - q.n;
+    return q;
+}
+__host__ __device__ inline int page_or_none(int id, int n_pages) { return id >= 0 && id < n_pages ? id : -1; }
+
+__device__ __forceinline__ Seq seq_at(const SeqArgs& a, int s) {
+    const int len = as_global(a.kv_len)[s];
+    if (!a.q_start) return seq_from(s, s + 1, len, a.n_tokens, a.max_kv);
+    return seq_from(as_global(a.q_start)[s], as_global(a.q_start)[s + 1], len, a.n_tokens, a.max_kv);
+}
+
+// The sequence of token t: the last one whose tokens begin at or before t (those without tokens in between are passed over).
+__device__ __forceinline__ int seq_of(const SeqArgs& a, int t) {
+    if (!a.q_start) return min(t, a.n_seqs - 1);
+    int lo = 0, hi = a.n_seqs - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (as_global(a.q_start)[mid] <= t) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+}  // namespace patch
