@@ -9,6 +9,8 @@
 // keys' side as the matrix instruction's A operand: S^T = K Q^T and O^T = V^T P^T.  A column is then a row of the attention, one column per lane in
 // both, and the second product's B operand is what the lane already holds of the first's result, if the keys of a step are given out to the rows of A
 // in the right order: no value of P crosses lanes.  V lies feature-major in its pages, so V^T's operand is a plain 16-byte load too.
+#include <algorithm>
+
 #include "cells.h"
 
 namespace patch {
@@ -27,6 +29,9 @@ __device__ __forceinline__ u32x4_t widen8(uint32_t lo, uint32_t hi) {
 }
 
 constexpr float kNone = -__builtin_inff();
+// The maximum that scores are held against follows the true one only where that is more than this above it (in powers of two): a p is then at most 2^8, which
+// costs neither bf16's relative step nor the fp32 sums anything, and after a row's first keys the sums hardly ever have to be scaled down.
+constexpr float kRise = 8.f;
 // exp2(x - m) where m may be the maximum of nothing
 __device__ __forceinline__ float exp2_off(float x, float m) { return __builtin_amdgcn_exp2f(x - (m == kNone ? 0.f : m)); }
 
@@ -103,7 +108,7 @@ __device__ __forceinline__ bool any_infinite(const u32x4_t& v) {      // or NaN
 
 // Few rows: each wavefront takes steps of 32 keys of its own, K and V straight from memory into the operands' registers, RB blocks of 16 rows against
 // them; the four wavefronts' results meet in LDS.
-constexpr int kTableKeys = 2048;   // page numbers of so many keys are in LDS at a time
+constexpr int kTableKeys = 4096;   // page numbers of so many keys are in LDS at a time
 
 template <int D, bool E4M3>
 struct KeyRegs {
@@ -155,7 +160,7 @@ template <bool E4M3>
 __device__ __forceinline__ int query_offset(int i, int g) { return E4M3 ? 64 * (i / 2) + 16 * g + 8 * (i % 2) : 32 * i + 8 * g; }
 
 template <int D, int RB, bool E4M3>
-__global__ __launch_bounds__(256) void attend_rows_kernel(const AttnArgs a, const int front) {
+__global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel(const AttnArgs a, const int front) {
     constexpr int kPitch = D + 4;
     __shared__ float sh_o[4][16][kPitch];
     __shared__ float sh_m[4][RB * 16], sh_l[4][RB * 16];
@@ -224,9 +229,13 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttnArgs a, cons
         }
         __syncthreads();
         const int* pages = sh_pages - (window >> a.cache.page_log2);
-        for (int step = window + 32 * wave; step < stop; step += 128) {
-            KeyRegs<D, E4M3> kv;
-            load_keys<D, E4M3>(kv, a, pages, step, kh, lane);
+        // the keys of a wavefront's next step are on their way while it works on one; behind its last it asks for that one again
+        KeyRegs<D, E4M3> next;
+        const int first_step = window + 32 * wave, last_step = first_step + (max(stop - 1 - first_step, 0) & ~127);
+        if (first_step < stop) load_keys<D, E4M3>(next, a, pages, first_step, kh, lane);
+        for (int step = first_step; step < stop; step += 128) {
+            const KeyRegs<D, E4M3> kv = next;
+            load_keys<D, E4M3>(next, a, pages, min(step + 128, last_step), kh, lane);
             f32x4_t s[RB][2];
 #pragma unroll
             for (int b = 0; b < RB; ++b) s[b][0] = s[b][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -242,7 +251,6 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttnArgs a, cons
                                 (pages[step >> a.cache.page_log2] | pages[(step + 16) >> a.cache.page_log2]) < 0;
             const int key = step + 8 * g;                       // the lane's eight keys
             bf16x8_t pr[RB];
-            float down[RB];
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
                 float x[8];
@@ -257,18 +265,22 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttnArgs a, cons
                 float top = x[0];
 #pragma unroll
                 for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float m_new = fmaxf(m[b], top);
-                down[b] = exp2_off(m[b], m_new);
-                m[b] = m_new;
+                if (__any(top > m[b] + kRise)) {
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    const float m_new = fmaxf(m[b], top), down = exp2_off(m[b], m_new);
+                    m[b] = m_new;
+                    l[b] *= down;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) o[b][i] = o[b][i] * down;
+                }
                 float sum = 0.f, y[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    y[e] = exp2_off(x[e], m_new);
+                    y[e] = exp2_off(x[e], m[b]);
                     sum += y[e];
                 }
-                l[b] = l[b] * down[b] + sum;
+                l[b] += sum;
                 pr[b] = as_bf16x8(u32x4_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])});
             }
             u32x4_t v[D / 16];
@@ -284,15 +296,16 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttnArgs a, cons
             }
             // ... and so may keys that only some of the rows see: those are then taken one by one, for the rows that see them
             if (ragged && fewest < min(step + 32, p.key1) && __any(infinite)) {
+#pragma unroll 1
                 for (int one = step; one < step + 32; ++one)
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i) {
+                        __builtin_amdgcn_sched_barrier(0);       // one operand at a time: this is rare, and registers are not
                         u32x4_t w = v[i];
                         keep_keys(w, key, one, one + 1);
 #pragma unroll
                         for (int b = 0; b < RB; ++b) {
                             const f32x4_t add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), pr[b], f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                            if (one == step) o[b][i] = o[b][i] * down[b];
                             if (one < limit[b]) o[b][i] = o[b][i] + add;
                         }
                     }
@@ -300,10 +313,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttnArgs a, cons
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        o[b][i] = o[b][i] * down[b];
-                        o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v[i]), pr[b], o[b][i], 0, 0, 0);
-                    }
+                    for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v[i]), pr[b], o[b][i], 0, 0, 0);
             }
         }
     }
@@ -368,40 +378,57 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(const AttnArgs a, cons
     }
 }
 
-// The parts of a row, added in their order: one wavefront a row.
+// The parts of a row: D / 4 threads hold a part's row, so that a workgroup's other threads take other parts; every load is there before one is needed.  Each
+// group of threads adds its parts in their order, then the groups' sums are added in theirs.
 template <int D>
 __global__ __launch_bounds__(256) void attend_merge_kernel(const AttnArgs a) {
-    const int64_t rows = (int64_t)a.seqs.n_tokens * a.heads;
-    const int64_t row = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const int lane = threadIdx.x & 63, t = (int)(row / a.heads), head = (int)(row % a.heads);
+    constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
+    __shared__ float sh_top[4], sh_sum[kGroups];
+    __shared__ f32x4_t sh_acc[kGroups][kLanes];
+    const int64_t rows = (int64_t)a.seqs.n_tokens * a.heads, row = (int64_t)blockIdx.x * a.heads + blockIdx.y;
+    const int t = blockIdx.x, head = blockIdx.y;
     const Seq q = seq_at(a.seqs, seq_of(a.seqs, t));
     if (t - q.first >= q.n) return;                           // no sequence has this token
     const int own = own_parts(a, q.len);
     if (a.prefix_parts == 0 && own <= 1) return;              // written by the workgroup itself
-    const int pos = q.pos0 + t - q.first;
+    // own parts behind the row's position are left out: nothing in them is seen
+    const int pos = q.pos0 + t - q.first, base = a.prefix & ~31;
+    const int parts = a.prefix_parts + (pos < base ? 0 : min(own, (pos - base) / a.own_chunk + 1));
     float top = kNone;
-    const int parts = a.prefix_parts + own;
-    constexpr int E = D / 64;
-    float acc[E] = {}, sum = 0.f;
-    for (int i = 0; i < parts; ++i) {
-        if (i >= a.prefix_parts && (a.prefix & ~31) + (i - a.prefix_parts) * a.own_chunk > pos) continue;   // sees none of its keys
+    for (int i = threadIdx.x; i < parts; i += 256) top = fmaxf(top, as_global(a.part_ml)[2 * (i * rows + row)]);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+    if ((threadIdx.x & 63) == 0) sh_top[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(sh_top[0], sh_top[1]), fmaxf(sh_top[2], sh_top[3]));
+    const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+#pragma unroll 4
+    for (int i = group; i < parts; i += kGroups) {
         const int64_t at = i * rows + row;
-        const float m = as_global(a.part_ml)[2 * at], l = as_global(a.part_ml)[2 * at + 1];
-        const float m_new = fmaxf(top, m), down = exp2_off(top, m_new), up = exp2_off(m, m_new);
-        top = m_new;
-        sum = sum * down + l * up;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = acc[e] * down + as_global(a.part_o)[at * D + lane * E + e] * up;
+        const float up = exp2_off(as_global(a.part_ml)[2 * at], top);
+        sum += as_global(a.part_ml)[2 * at + 1] * up;
+        acc += *reinterpret_cast<const PATCH_EP_GLOBAL f32x4_t*>(as_global(a.part_o) + at * D + 4 * lane) * up;
     }
-    const float over = q.bad ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum;
-    uint16_t* O = a.O + t * a.o_stride + (int64_t)head * D + lane * E;
+    sh_acc[group][lane] = acc;
+    if (lane == 0) sh_sum[group] = sum;
+    __syncthreads();
+    if (group != 0) return;
 #pragma unroll
-    for (int e = 0; e < E; ++e) as_global_out(O)[e] = (uint16_t)bf16_rne_bits(acc[e] * over);
+    for (int i = 1; i < kGroups; ++i) {
+        acc += sh_acc[i][lane];
+        sum += sh_sum[i];
+    }
+    acc *= q.bad ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum;
+    *reinterpret_cast<PATCH_EP_GLOBAL u32x2_t*>(as_global_out(a.O) + t * a.o_stride + (int64_t)head * D + 4 * lane) =
+        u32x2_t{bf16_pair(acc[0], acc[1]), bf16_pair(acc[2], acc[3])};
     if (a.lse && lane == 0) as_global_out(a.lse)[row] = 0.6931471805599453f * (top + __builtin_log2f(sum));
 }
 
-// workgroups in a launch's x direction: far from the 2^32 threads that one may have (groups of rows alone are at most 2^21 of them)
+// Workgroups that a launch over keys is split into: two on each compute unit, all of them there at once.  One sequence of 65000 keys, 8 key heads of 128:
+// 512 workgroups 56.5 us, 1024 62.2; 64 rows behind 8192 shared keys 109 and 154; 29 ragged sequences of up to 8000 64.6 and 65.3.
+constexpr int64_t kWanted = 512;
 constexpr int64_t kMostGroups = (int64_t)1 << 22;
 
 static inline int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -417,17 +444,15 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     const int base = a->prefix & ~31;
     const int own = a->seqs.max_kv - base;
     int64_t units = (int64_t)a->seqs.n_seqs * a->cache.kv_heads * ((a->seqs.max_q * a->group + 63) / 64);
-    int64_t chunks = (1024 + units - 1) / units;
-    int64_t chunk = up_to((own + chunks - 1) / chunks, 128);
+    int64_t chunk = up_to((own * units + kWanted - 1) / kWanted, 128);
     if (chunk < 256) chunk = 256;
-    if (chunk > 2048) chunk = 2048;
+    if (chunk > 4096) chunk = 4096;
     const int64_t groups = ((int64_t)a->seqs.max_q * a->group + 15) / 16;
     if (own / chunk * groups > kMostGroups) chunk = up_to(own / (kMostGroups / groups), 128);
     int64_t prefix_parts = 0;
     if (a->prefix) {
         units = (int64_t)a->cache.kv_heads * (((int64_t)a->seqs.n_tokens * a->group + 63) / 64);
-        chunks = (1024 + units - 1) / units;
-        a->prefix_chunk = (int)up_to((a->prefix + chunks - 1) / chunks, 128);
+        a->prefix_chunk = (int)up_to(std::min<int64_t>((a->prefix * units + kWanted - 1) / kWanted, a->prefix), 128);
         if (a->prefix_chunk < 256) a->prefix_chunk = 256;
         prefix_parts = (a->prefix + a->prefix_chunk - 1) / a->prefix_chunk;
         if (prefix_parts > most / 2) {
@@ -448,20 +473,27 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
 }
 
 template <int D, int RB, bool E4M3>
-static void launch_rows(const AttnArgs& a, hipStream_t stream) {
-    const auto groups = [&](int tokens) { return (unsigned)(((int64_t)tokens * a.group + 16 * RB - 1) / (16 * RB)); };
-    const unsigned kv = (unsigned)a.cache.kv_heads;
-    if (a.prefix_parts) attend_rows_kernel<D, RB, E4M3><<<dim3(a.prefix_parts * groups(a.seqs.n_tokens), kv), 256, 0, stream>>>(a, 1);
-    attend_rows_kernel<D, RB, E4M3><<<dim3((a.parts - a.prefix_parts) * groups(a.seqs.max_q), kv, (unsigned)a.seqs.n_seqs), 256, 0, stream>>>(a, 0);
+static void launch_rows(const AttnArgs& a, int front, hipStream_t stream) {
+    const int tokens = front ? a.seqs.n_tokens : a.seqs.max_q, parts = front ? a.prefix_parts : a.parts - a.prefix_parts;
+    const unsigned groups = (unsigned)(((int64_t)tokens * a.group + 16 * RB - 1) / (16 * RB));
+    attend_rows_kernel<D, RB, E4M3><<<dim3(parts * groups, (unsigned)a.cache.kv_heads, front ? 1u : (unsigned)a.seqs.n_seqs), 256, 0, stream>>>(a, front);
+}
+
+template <int D, bool E4M3>
+static void launch_rows_of(const AttnArgs& a, hipStream_t stream) {
+    for (int front = a.prefix_parts ? 1 : 0; front >= 0; --front) {
+        const int64_t rows = (int64_t)(front ? a.seqs.n_tokens : a.seqs.max_q) * a.group;
+        if (rows <= 16 || D == 256) launch_rows<D, 1, E4M3>(a, front, stream);
+        else launch_rows<D, D == 256 ? 1 : 2, E4M3>(a, front, stream);
+    }
 }
 
 template <int D>
 static void launch_d(const AttnArgs& a, hipStream_t stream) {
-    if (a.cache.e4m3) launch_rows<D, 2, true>(a, stream);
-    else launch_rows<D, 2, false>(a, stream);
+    if (a.cache.e4m3) launch_rows_of<D, true>(a, stream);
+    else launch_rows_of<D, false>(a, stream);
     if (a.parts > 1) {
-        const int64_t rows = (int64_t)a.seqs.n_tokens * a.heads;
-        attend_merge_kernel<D><<<(unsigned)((rows + 3) / 4), 256, 0, stream>>>(a);
+        attend_merge_kernel<D><<<dim3((unsigned)a.seqs.n_tokens, (unsigned)a.heads), 256, 0, stream>>>(a);
     }
 }
 

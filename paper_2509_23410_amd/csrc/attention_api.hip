@@ -141,7 +141,7 @@ patch_status patch_kv_append(const patch_heads* k, const patch_heads* v, const p
 }
 
 static patch_status fill_attention(AttnArgs* a, int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const patch_attention_opts* opts) {
-    if (!seqs || !cache || heads < 1 || heads > (1 << 16)) return PATCH_ERR_ARG;
+    if (!seqs || !cache || heads < 1 || heads > 65535) return PATCH_ERR_ARG;
     TRY(fill_cache(&a->cache, cache));
     TRY(fill_seqs(&a->seqs, seqs, cache->page_size));
     if (heads % cache->kv_heads) return PATCH_ERR_SHAPE;
