@@ -106,6 +106,64 @@ __device__ __forceinline__ bool any_infinite(const u32x4_t& v) {      // or NaN
     return any;
 }
 
+__device__ __forceinline__ float cell_value(const uint8_t* base, int64_t i, bool e4m3) {
+    if (e4m3) return __builtin_amdgcn_cvt_f32_fp8((int)as_global(base)[i], 0);
+    return __uint_as_float((uint32_t)reinterpret_cast<const PATCH_EP_GLOBAL uint16_t*>(as_global(base))[i] << 16);
+}
+
+// One row by one wavefront, key by key and with no key that the row does not see.  In the products of the kernels below a row has 0 times the values of the
+// keys behind it, which is a NaN where those are not finite: workgroups that come across such values do their rows again here.  Slow, and hardly ever run.
+template <int D, bool E4M3>
+__device__ __forceinline__ void attend_row_alone(const AttnArgs& a, const Span& p, int kh, int r, int lane) {
+    constexpr int E = D / 64;
+    const int limit = row_limit(a, p, r), mask = (1 << a.cache.page_log2) - 1;
+    const int64_t token = p.t0 + r / a.group;
+    const int head = kh * a.group + r % a.group;
+    float q[E], acc[E], m = kNone, l = 0.f, scale = a.scale, v_scale = 1.f;
+    if (E4M3 && a.cache.k_scale) scale *= as_global(a.cache.k_scale)[kh];
+    if (E4M3 && a.cache.v_scale) v_scale = as_global(a.cache.v_scale)[kh];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        q[e] = cell_value(reinterpret_cast<const uint8_t*>(a.Q), token * a.q_stride + (int64_t)head * D + lane * E + e, false);
+        acc[e] = 0.f;
+    }
+#pragma unroll 1
+    for (int key = max(p.begin, p.key0); key < min(p.end, limit); ++key) {
+        const int id = p.bad ? -1 : page_or_none(as_global(a.seqs.table)[p.table + (key >> a.cache.page_log2)], a.cache.n_pages);
+        float s = 0.f, v[E];
+        const int64_t cells = (int64_t)kh << a.cache.page_log2;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int d = lane * E + e;
+            s += q[e] * cell_value(a.cache.k + max(id, 0) * a.cache.page_bytes, (cells + (key & mask)) * D + d, E4M3);
+            v[e] = cell_value(a.cache.v + max(id, 0) * a.cache.page_bytes, cells * D + ((int64_t)d << a.cache.page_log2) + (key & mask), E4M3);
+        }
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) s += __shfl_xor(s, x);
+        s = id < 0 ? __builtin_nanf("") : s * scale;
+        const float m_new = fmaxf(m, s), down = exp2_off(m, m_new), up = exp2_off(s, m_new);
+        m = m_new;
+        l = l * down + up;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = acc[e] * down + v[e] * up;
+    }
+    const int64_t row = token * a.heads + head, part = (int64_t)p.part * a.seqs.n_tokens * a.heads + row;
+    const float over = (p.part < 0 ? (l == 0.f ? 0.f : 1.f / l) : 1.f) * v_scale;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if (p.part < 0) as_global_out(a.O)[token * a.o_stride + (int64_t)head * D + lane * E + e] = (uint16_t)bf16_rne_bits(acc[e] * over);
+        else as_global_out(a.part_o)[part * D + lane * E + e] = acc[e] * over;
+    }
+    if (lane == 0) {
+        if (p.part >= 0) {
+            as_global_out(a.part_ml)[2 * part] = m;
+            as_global_out(a.part_ml)[2 * part + 1] = l;
+        } else if (a.lse) {
+            as_global_out(a.lse)[row] = 0.6931471805599453f * (m + __builtin_log2f(l));
+        }
+    }
+}
+
 // Few rows: each wavefront takes steps of 32 keys of its own, K and V straight from memory into the operands' registers, RB blocks of 16 rows against
 // them; the four wavefronts' results meet in LDS.
 constexpr int kTableKeys = 4096;   // page numbers of so many keys are in LDS at a time
@@ -214,6 +272,7 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
         for (int i = 0; i < D / 16; ++i) o[b][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
 
+    bool redo = false;
     for (int window = p.begin; window < end; window += kTableKeys) {
         const int stop = min(end, window + kTableKeys);
         // page numbers, as steps of 32 keys may touch them: -1 where there is none or it is out of range
@@ -294,28 +353,17 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
                     infinite |= any_infinite(v[i]);
                 }
             }
-            // ... and so may keys that only some of the rows see: those are then taken one by one, for the rows that see them
-            if (ragged && fewest < min(step + 32, p.key1) && __any(infinite)) {
-#pragma unroll 1
-                for (int one = step; one < step + 32; ++one)
+            // ... and so may keys that only some of the rows see
+            redo |= ragged && fewest < min(step + 32, p.key1) && infinite;
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        __builtin_amdgcn_sched_barrier(0);       // one operand at a time: this is rare, and registers are not
-                        u32x4_t w = v[i];
-                        keep_keys(w, key, one, one + 1);
+            for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                        for (int b = 0; b < RB; ++b) {
-                            const f32x4_t add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), pr[b], f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                            if (one < limit[b]) o[b][i] = o[b][i] + add;
-                        }
-                    }
-            } else {
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                    for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v[i]), pr[b], o[b][i], 0, 0, 0);
-            }
+                for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v[i]), pr[b], o[b][i], 0, 0, 0);
         }
+    }
+    if (__syncthreads_or(redo)) {
+        for (int r = first_row + wave; r < min(first_row + 16 * RB, p.rows); r += 4) attend_row_alone<D, E4M3>(a, p, kh, r, lane);
+        return;
     }
 
     // the four wavefronts' results: rows of a block of 16 at a time, 16 threads a row
@@ -378,6 +426,243 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
     }
 }
 
+// Many rows: a workgroup's wavefronts have 32 rows each, and the keys come through LDS for all of them, kTile at a time, the next ones on their way through
+// registers meanwhile.  The products are the ones above on 32 x 32 x 16 instructions.
+constexpr int kTile = 64;
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+// Where 16-byte chunk c of a row lies in LDS: rows of 8 (or 16 and more) chunks, 16 rows in a row's reading order never meet in a bank
+template <int CHUNKS>
+__device__ __forceinline__ int chunk_at(int row, int c) {
+    return row * CHUNKS + (CHUNKS == 8 ? c ^ ((row + (row >> 3)) & 7) : c ^ (row & 15));
+}
+// The row of the K tile that key i of 32 is in: a lane's eight values of P in the order of the second product's operand (bits 2 and 3 change places)
+__device__ __forceinline__ int key_row(int i) { return (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1); }
+
+template <int D, int NW, bool E4M3>
+__global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void attend_tiles_kernel(const AttnArgs a, const int front) {
+    constexpr int kThreads = 64 * NW, kCells = E4M3 ? 16 : 8;                  // of a 16-byte load
+    constexpr int kLoads = kTile * D / kCells, kEach = (kLoads + kThreads - 1) / kThreads;
+    constexpr int kRowLoads = D / kCells, kKeyLoads = kTile / kCells;          // of a key, of a feature
+    static_assert(kThreads % kRowLoads == 0 && kThreads % kKeyLoads == 0 && (kLoads % kThreads == 0 || kLoads < kThreads), "staging");
+    __shared__ u32x4_t sh_k[2][kTile * D / 8], sh_v[2][kTile * D / 8];
+    __shared__ int sh_infinite[2][NW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
+    // key heads are the fastest index: with 8 of them, or 16 and so on, each die has heads of its own, and those in its L2
+    const int kh = blockIdx.x % a.cache.kv_heads, rest = blockIdx.x / a.cache.kv_heads;
+    const int groups = ((front ? a.seqs.n_tokens : a.seqs.max_q) * a.group + 32 * NW - 1) / (32 * NW);
+    const int chunk = rest / groups, first_row = (groups - 1 - rest % groups) * (32 * NW);       // the rows that see most first
+    const Span p = front ? front_span(a, chunk) : own_span(a, blockIdx.y, chunk);
+    if (first_row >= p.rows) return;
+    if (p.begin >= p.end && (p.part >= 0 || chunk > 0)) return;
+
+    const int r = first_row + 32 * wave + col;
+    const bool there = r < p.rows;
+    const int limit = row_limit(a, p, r);
+    int fewest = there ? limit : 0x7FFFFFFF, most = limit;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+        fewest = min(fewest, __shfl_xor(fewest, m));
+        most = max(most, __shfl_xor(most, m));
+    }
+    fewest = __builtin_amdgcn_readfirstlane(fewest);
+    most = __builtin_amdgcn_readfirstlane(most);
+    // keys up to the last one that any row of the workgroup sees
+    const int end = front ? p.end : min(p.end, p.pos0 + min(first_row + 32 * NW - 1, p.rows - 1) / a.group + 1);
+
+    const int64_t q_at = there ? (int64_t)(p.t0 + r / a.group) * a.q_stride + (int64_t)(kh * a.group + r % a.group) * D : 0;
+    bf16x8_t q[D / 16];
+    const uint32_t turn = a.scale < 0.f ? 0x80008000u : 0u;                    // so that the largest product is the largest score
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        u32x4_t v = {0, 0, 0, 0};
+        if (there) v = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(a.Q) + q_at + 16 * i + 8 * h) ^ turn;
+        q[i] = as_bf16x8(v);
+    }
+    float scale = a.scale < 0.f ? -a.scale : a.scale;
+    if (E4M3 && a.cache.k_scale) scale *= as_global(a.cache.k_scale)[kh];
+
+    f32x16_t o[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    float m = kNone, l = 0.f;
+    bool redo = false;
+
+    // staging: thread's key rows of K (one per load) and keys of V (the same for all its loads)
+    const int page_mask = (1 << a.cache.page_log2) - 1;
+    const int k_row = tid / kRowLoads, k_chunk = tid % kRowLoads, v_row = tid / kKeyLoads, v_key = (tid % kKeyLoads) * kCells;
+    constexpr int kRowStep = kThreads / kRowLoads, kFeatureStep = kThreads / kKeyLoads;
+    int k_page[kEach], v_page;
+    u32x4_t k_regs[kEach], v_regs[kEach];
+    int k_from[kEach], v_from;                                                 // the pages that the registers' keys are of
+    const auto page_of = [&](int key) {
+        int id = -1;
+        if (key < p.key1 && !p.bad) id = page_or_none(as_global(a.seqs.table)[p.table + (key >> a.cache.page_log2)], a.cache.n_pages);
+        return id;
+    };
+    const auto ask_pages = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) k_page[i] = page_of(tile + k_row + i * kRowStep);
+        v_page = page_of(tile + v_key);
+    };
+    const auto ask_keys = [&](int tile) {
+        if (kLoads < kThreads && tid >= kLoads) return;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int key = tile + k_row + i * kRowStep;
+            k_from[i] = k_page[i];
+            k_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(a.cache.k) + max(k_page[i], 0) * a.cache.page_bytes +
+                                                                         ((((int64_t)kh << a.cache.page_log2) + (key & page_mask)) * D + k_chunk * kCells) * (16 / kCells));
+        }
+        v_from = v_page;
+        const PATCH_EP_GLOBAL uint8_t* base = as_global(a.cache.v) + max(v_page, 0) * a.cache.page_bytes;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            v_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(base + ((((int64_t)kh * D + v_row + i * kFeatureStep) << a.cache.page_log2) + ((tile + v_key) & page_mask)) * (16 / kCells));
+    };
+    const auto put_keys = [&](int tile, int buffer) {
+        bool infinite = false;
+        if (kLoads >= kThreads || tid < kLoads) {
+            const bool edge = tile < p.key0 || tile + kTile > p.key1;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int at = k_row + i * kRowStep, row = (at & ~31) | key_row(at & 31), feature = v_row + i * kFeatureStep;
+                u32x4_t k[2], v[2];
+                if constexpr (E4M3) {
+                    k[0] = widen8(k_regs[i][0], k_regs[i][1]), k[1] = widen8(k_regs[i][2], k_regs[i][3]);
+                    v[0] = widen8(v_regs[i][0], v_regs[i][1]), v[1] = widen8(v_regs[i][2], v_regs[i][3]);
+                } else {
+                    k[0] = k_regs[i], v[0] = v_regs[i];
+                }
+                constexpr int kParts = kCells / 8;
+#pragma unroll
+                for (int b = 0; b < kParts; ++b) {
+                    if (k_from[i] < 0) k[b] = u32x4_t{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};      // a page that is not there: NaN scores
+                    if (v_from < 0) v[b] = u32x4_t{0, 0, 0, 0};
+                    if (edge) keep_keys(v[b], tile + v_key + 8 * b, p.key0, p.key1);                             // cells that no key is in
+                    infinite |= any_infinite(v[b]);
+                    sh_k[buffer][chunk_at<D / 8>(row, k_chunk * kParts + b)] = k[b];
+                    sh_v[buffer][chunk_at<kTile / 8>(feature, v_key / 8 + b)] = v[b];
+                }
+            }
+        }
+        infinite = __any(infinite);
+        if (lane == 0) sh_infinite[buffer][wave] = infinite;
+    };
+
+    if (p.begin < end) {
+        ask_pages(p.begin);
+        ask_keys(p.begin);
+        ask_pages(p.begin + kTile);
+        put_keys(p.begin, 0);
+        __syncthreads();
+    }
+    int buffer = 0;
+    for (int tile = p.begin; tile < end; tile += kTile, buffer ^= 1) {
+        const bool more = tile + kTile < end;
+        if (more) {
+            ask_keys(tile + kTile);
+            ask_pages(tile + 2 * kTile);
+        }
+        if (tile < most) {
+            f32x16_t s[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh_k[buffer][chunk_at<D / 8>(32 * b + col, 2 * i + h)]), q[i], s[b], 0, 0, 0);
+            const bool ragged = tile < p.key0 || tile + kTile > fewest;
+            if (ragged) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int key = tile + 32 * b + 16 * (e / 8) + 8 * h + e % 8;
+                        if (key < p.key0 || key >= limit) s[b][e] = kNone;
+                    }
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
+            top = top == kNone ? kNone : top * scale;                          // (a scale of zero makes no NaN of it)
+            if (__any(top > m + kRise)) {
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float m_new = fmaxf(m, top), down = exp2_off(m, m_new);
+                m = m_new;
+                l *= down;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) o[i] = o[i] * down;
+            }
+            const float off = m == kNone ? 0.f : m;
+            bf16x8_t pr[4];
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 2][8 * (k % 2) + e], scale, -off));
+                    sum[k] += y[e];
+                }
+                pr[k] = as_bf16x8(u32x4_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])});
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            if (ragged && fewest < min(tile + kTile, p.key1)) {                // keys that only some of the rows see, and not finite?
+#pragma unroll
+                for (int w = 0; w < NW; ++w) redo |= sh_infinite[buffer][w] != 0;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i)
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh_v[buffer][chunk_at<kTile / 8>(32 * i + col, 2 * k + h)]), pr[k], o[i], 0, 0, 0);
+        }
+        if (more) put_keys(tile + kTile, buffer ^ 1);
+        __syncthreads();
+    }
+
+    if (__syncthreads_or(redo)) {
+        for (int r1 = first_row + wave; r1 < min(first_row + 32 * NW, p.rows); r1 += NW) attend_row_alone<D, E4M3>(a, p, kh, r1, lane);
+        return;
+    }
+    l += __shfl_xor(l, 32);
+    if (!there) return;
+    float v_scale = 1.f;
+    if (E4M3 && a.cache.v_scale) v_scale = as_global(a.cache.v_scale)[kh];
+    const int64_t token = p.t0 + r / a.group;
+    const int head = kh * a.group + r % a.group;
+    const int64_t row = token * a.heads + head;
+    if (p.part < 0) {
+        const float over = (l == 0.f ? 0.f : 1.f / l) * v_scale;
+        const int64_t at = token * a.o_stride + (int64_t)head * D + 4 * h;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<PATCH_EP_GLOBAL u32x2_t*>(as_global_out(a.O) + at + 32 * i + 2 * e) =
+                    u32x2_t{bf16_pair(o[i][e] * over, o[i][e + 1] * over), bf16_pair(o[i][e + 2] * over, o[i][e + 3] * over)};
+        if (a.lse && h == 0) as_global_out(a.lse)[row] = 0.6931471805599453f * (m + __builtin_log2f(l));
+    } else {
+        const int64_t at = (int64_t)p.part * a.seqs.n_tokens * a.heads + row;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<PATCH_EP_GLOBAL f32x4_t*>(as_global_out(a.part_o) + at * D + 4 * h + 32 * i + 2 * e) =
+                    f32x4_t{o[i][e] * v_scale, o[i][e + 1] * v_scale, o[i][e + 2] * v_scale, o[i][e + 3] * v_scale};
+        if (h == 0) {
+            as_global_out(a.part_ml)[2 * at] = m;
+            as_global_out(a.part_ml)[2 * at + 1] = l;
+        }
+    }
+}
+
 // The parts of a row: D / 4 threads hold a part's row, so that a workgroup's other threads take other parts; every load is there before one is needed.  Each
 // group of threads adds its parts in their order, then the groups' sums are added in theirs.
 template <int D>
@@ -426,41 +711,51 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const AttnArgs a) {
     if (a.lse && lane == 0) as_global_out(a.lse)[row] = 0.6931471805599453f * (top + __builtin_log2f(sum));
 }
 
-// Workgroups that a launch over keys is split into: two on each compute unit, all of them there at once.  One sequence of 65000 keys, 8 key heads of 128:
-// 512 workgroups 56.5 us, 1024 62.2; 64 rows behind 8192 shared keys 109 and 154; 29 ragged sequences of up to 8000 64.6 and 65.3.
-constexpr int64_t kWanted = 512;
-constexpr int64_t kMostGroups = (int64_t)1 << 22;
+// Which kernel takes so many rows of a key head (those of a sequence, or of all in the shared front), as the rows of a workgroup.
+static int rows_of_block(int64_t rows, int head_dim) {
+    if (rows <= 16) return 16;
+    if (rows <= 32 && head_dim <= 128) return 32;
+    return rows <= 128 || head_dim == 256 ? 128 : 256;
+}
+
+// Keys that a workgroup takes, so that a launch over `keys` of them for `units` sequences, key heads and blocks of rows is two workgroups of four wavefronts
+// on each compute unit (or one of eight), all of them there at once.  One sequence of 65000 keys, 8 key heads of 128: 512 workgroups 56.5 us, 1024 62.2;
+// 64 rows behind 8192 shared keys 109 and 154; 29 ragged sequences of up to 8000 64.6 and 65.3.  Where that is a whole batch at decoding the longest is cut up
+// all the same, as the others may be shorter.
+static int64_t chunk_of(int64_t keys, int64_t units, int block, int64_t grid_units) {
+    constexpr int64_t kMostGroups = (int64_t)1 << 22;         // workgroups in x: far from the 2^32 threads that one may have there
+    const int64_t wanted = block == 256 ? 256 : 512, least = 256, most = block <= 32 ? 4096 : keys;
+    int64_t chunk = (keys * units + wanted - 1) / wanted;
+    chunk = std::min(std::max(chunk, least), std::max(most, least));
+    if (keys / chunk > kMostGroups / grid_units) chunk = keys / std::max<int64_t>(kMostGroups / grid_units, 1) + 1;
+    return (chunk + 127) / 128 * 128;
+}
 
 static inline int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
+    const int D = a->cache.head_dim, heads = a->cache.kv_heads;
     const int64_t rows = (int64_t)a->seqs.n_tokens * a->heads;
-    const size_t per_part = (size_t)rows * (a->cache.head_dim + 2) * 4;
+    const size_t per_part = (size_t)rows * (D + 2) * 4;
     const int64_t most = ws_bytes < 16 ? 0 : (int64_t)((ws_bytes - 16) / per_part);      // parts that the workspace holds
     a->prefix_parts = 0;
     a->parts = 1;
     if (a->prefix > a->seqs.max_kv) a->prefix = a->seqs.max_kv;
     if (most < 2 || a->seqs.n_seqs < 2) a->prefix = 0;        // every sequence reads the shared keys as its own
-    const int base = a->prefix & ~31;
-    const int own = a->seqs.max_kv - base;
-    int64_t units = (int64_t)a->seqs.n_seqs * a->cache.kv_heads * ((a->seqs.max_q * a->group + 63) / 64);
-    int64_t chunk = up_to((own * units + kWanted - 1) / kWanted, 128);
-    if (chunk < 256) chunk = 256;
-    if (chunk > 4096) chunk = 4096;
-    const int64_t groups = ((int64_t)a->seqs.max_q * a->group + 15) / 16;
-    if (own / chunk * groups > kMostGroups) chunk = up_to(own / (kMostGroups / groups), 128);
+    const auto blocks = [&](int64_t tokens, int block) { return (tokens * a->group + block - 1) / block; };
     int64_t prefix_parts = 0;
     if (a->prefix) {
-        units = (int64_t)a->cache.kv_heads * (((int64_t)a->seqs.n_tokens * a->group + 63) / 64);
-        a->prefix_chunk = (int)up_to(std::min<int64_t>((a->prefix * units + kWanted - 1) / kWanted, a->prefix), 128);
-        if (a->prefix_chunk < 256) a->prefix_chunk = 256;
-        prefix_parts = (a->prefix + a->prefix_chunk - 1) / a->prefix_chunk;
-        if (prefix_parts > most / 2) {
-            a->prefix_chunk = (int)up_to((a->prefix + most / 2 - 1) / (most / 2), 128);
-            prefix_parts = (a->prefix + a->prefix_chunk - 1) / a->prefix_chunk;
-        }
+        const int block = rows_of_block((int64_t)a->seqs.n_tokens * a->group, D);
+        const int64_t units = blocks(a->seqs.n_tokens, block) * heads;
+        int64_t chunk = chunk_of(a->prefix, units, block, units);
+        if ((a->prefix + chunk - 1) / chunk > most / 2) chunk = up_to((a->prefix + most / 2 - 1) / (most / 2), 128);
+        a->prefix_chunk = (int)chunk;
+        prefix_parts = (a->prefix + chunk - 1) / chunk;
     }
-    const int64_t left = most - prefix_parts;
+    const int64_t own = a->seqs.max_kv - (a->prefix & ~31), left = most - prefix_parts;
+    const int block = rows_of_block((int64_t)a->seqs.max_q * a->group, D);
+    const int64_t units = blocks(a->seqs.max_q, block) * heads;
+    int64_t chunk = chunk_of(own, units * a->seqs.n_seqs, block, units);
     if (left < 2 && !a->prefix) chunk = up_to(own > 0 ? own : 1, 128);
     else if ((own + chunk - 1) / chunk > left) chunk = up_to((own + left - 1) / left, 128);
     a->own_chunk = (int)chunk;
@@ -469,7 +764,7 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     a->parts = (int)(prefix_parts + own_most);
     if (a->parts == 1) return 0;
     a->part_o = a->part_ml + 2 * up_to(a->parts * rows, 2);
-    return (size_t)(2 * up_to(a->parts * rows, 2) + (int64_t)a->parts * rows * a->cache.head_dim) * 4;
+    return (size_t)(2 * up_to(a->parts * rows, 2) + (int64_t)a->parts * rows * D) * 4;
 }
 
 template <int D, int RB, bool E4M3>
@@ -479,12 +774,21 @@ static void launch_rows(const AttnArgs& a, int front, hipStream_t stream) {
     attend_rows_kernel<D, RB, E4M3><<<dim3(parts * groups, (unsigned)a.cache.kv_heads, front ? 1u : (unsigned)a.seqs.n_seqs), 256, 0, stream>>>(a, front);
 }
 
+template <int D, int NW, bool E4M3>
+static void launch_tiles(const AttnArgs& a, int front, hipStream_t stream) {
+    const int tokens = front ? a.seqs.n_tokens : a.seqs.max_q, parts = front ? a.prefix_parts : a.parts - a.prefix_parts;
+    const unsigned groups = (unsigned)(((int64_t)tokens * a.group + 32 * NW - 1) / (32 * NW));
+    attend_tiles_kernel<D, NW, E4M3><<<dim3(parts * groups * (unsigned)a.cache.kv_heads, front ? 1u : (unsigned)a.seqs.n_seqs), 64 * NW, 0, stream>>>(a, front);
+}
+
 template <int D, bool E4M3>
 static void launch_rows_of(const AttnArgs& a, hipStream_t stream) {
     for (int front = a.prefix_parts ? 1 : 0; front >= 0; --front) {
-        const int64_t rows = (int64_t)(front ? a.seqs.n_tokens : a.seqs.max_q) * a.group;
-        if (rows <= 16 || D == 256) launch_rows<D, 1, E4M3>(a, front, stream);
-        else launch_rows<D, D == 256 ? 1 : 2, E4M3>(a, front, stream);
+        const int block = rows_of_block((int64_t)(front ? a.seqs.n_tokens : a.seqs.max_q) * a.group, D);
+        if (block == 16) launch_rows<D, 1, E4M3>(a, front, stream);
+        else if (block == 32) launch_rows<D, D == 256 ? 1 : 2, E4M3>(a, front, stream);
+        else if (block == 128) launch_tiles<D, 4, E4M3>(a, front, stream);
+        else launch_tiles<D, D == 256 ? 4 : 8, E4M3>(a, front, stream);
     }
 }
 
