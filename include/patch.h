@@ -468,7 +468,8 @@ typedef struct {
     void* k;                 /* DEVICE, 16-byte aligned                                                                          */
     void* v;                 /* DEVICE, 16-byte aligned                                                                          */
     int64_t n_pages;         /* up to 2^31 - 1                                                                                   */
-    int64_t page_stride;     /* cells from one page to the next, in k and in v, a multiple of 16; 0: pages lie side by side      */
+    int64_t page_stride;     /* cells from one page to the next, in k and in v, a multiple of 16, less than 4 GB of them; 0: pages */
+                             /* lie side by side                                                                                 */
     int page_size;           /* tokens: 16, 32, 64, 128 or 256                                                                   */
     int kv_heads, head_dim;  /* head_dim: 64, 128 or 256                                                                         */
     int e4m3;                /* 1: e4m3 cells, 0: bf16                                                                           */
@@ -519,7 +520,7 @@ typedef struct {
 /* O[t, h] = sum_j softmax_j(scale q[t, h] . k[j, h / (heads / kv_heads)]) v[j, ...] over the keys j at or before the token's
  * position in its sequence.
  *   Q  DEVICE, bf16, n_tokens rows of heads x head_dim, q_stride elements apart (a multiple of 8); heads a multiple of kv_heads
- *   O  DEVICE, bf16, the same with o_stride; Q itself may be O
+ *   O  DEVICE, bf16, the same with o_stride; not Q, nor may its rows overlap Q's
  * A row with no keys becomes zeros (lse: minus infinity).  Rows of tokens that no sequence has are left as they are.
  * Scores and sums are fp32; a probability is rounded to bf16 before it multiplies V, the result once at the end.
  * Cells of pages that hold no token yet may hold anything.

@@ -113,8 +113,9 @@ __device__ __forceinline__ float cell_value(const uint8_t* base, int64_t i, bool
 
 // One row by one wavefront, key by key and with no key that the row does not see.  In the products of the kernels below a row has 0 times the values of the
 // keys behind it, which is a NaN where those are not finite: workgroups that come across such values do their rows again here.  Slow, and hardly ever run.
+// It writes `features` of the head from `first` on, its sums held against *against (null: against the row's maximum), so that another workgroup's others fit.
 template <int D, bool E4M3>
-__device__ __forceinline__ void attend_row_alone(const AttnArgs& a, const Span& p, int kh, int r, int lane) {
+__device__ __forceinline__ void attend_row_alone(const AttnArgs& a, const Span& p, int kh, int r, int lane, const float* against, int first, int features) {
     constexpr int E = D / 64;
     const int limit = row_limit(a, p, r), mask = (1 << a.cache.page_log2) - 1;
     const int64_t token = p.t0 + r / a.group;
@@ -147,7 +148,15 @@ __device__ __forceinline__ void attend_row_alone(const AttnArgs& a, const Span& 
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = acc[e] * down + v[e] * up;
     }
+    if (against) {
+        const float held = *against, move = exp2_off(m, held);
+        m = held;
+        l *= move;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] *= move;
+    }
     const int64_t row = token * a.heads + head, part = (int64_t)p.part * a.seqs.n_tokens * a.heads + row;
+    if (lane * E < first || lane * E >= first + features) return;
     const float over = (p.part < 0 ? (l == 0.f ? 0.f : 1.f / l) : 1.f) * v_scale;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -167,6 +176,22 @@ __device__ __forceinline__ void attend_row_alone(const AttnArgs& a, const Span& 
 // Few rows: each wavefront takes steps of 32 keys of its own, K and V straight from memory into the operands' registers, RB blocks of 16 rows against
 // them; the four wavefronts' results meet in LDS.
 constexpr int kTableKeys = 4096;   // page numbers of so many keys are in LDS at a time
+
+// Page numbers of the keys [window, stop) and on to a multiple of 64 of them, -1 where there is none or it is out of range; window is a multiple of 32 and
+// stop at most kTableKeys behind it.  Whether a key of the span is without a page.
+__device__ __forceinline__ bool load_pages(const AttnArgs& a, const Span& p, int* to, int window, int stop) {
+    const int page0 = window >> a.cache.page_log2, last = window + ((stop - window + 63) & ~63) - 1, count = (last >> a.cache.page_log2) - page0 + 1;
+    bool none = false;
+    if ((int)threadIdx.x < count) {                              // at most kTableKeys / 16, of 256 threads or more
+        const int64_t i = page0 + (int)threadIdx.x;
+        const bool there = (i << a.cache.page_log2) < p.key1 && i < a.seqs.table_stride;
+        int id = -1;
+        if (there && !p.bad) id = page_or_none(as_global(a.seqs.table)[p.table + i], a.cache.n_pages);
+        to[threadIdx.x] = id;
+        none = there && id < 0;
+    }
+    return none;
+}
 
 template <int D, bool E4M3>
 struct KeyRegs {
@@ -277,15 +302,7 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
         const int stop = min(end, window + kTableKeys);
         // page numbers, as steps of 32 keys may touch them: -1 where there is none or it is out of range
         if (window != p.begin) __syncthreads();
-        {
-            const int page0 = window >> a.cache.page_log2, last = window + ((stop - window + 31) & ~31) - 1;
-            if ((int)threadIdx.x <= (last >> a.cache.page_log2) - page0) {     // at most kTableKeys / 16 of them: window is a multiple of 32
-                const int64_t i = page0 + (int)threadIdx.x;
-                int id = -1;
-                if (i * (1 << a.cache.page_log2) < p.key1 && i < a.seqs.table_stride) id = as_global(a.seqs.table)[p.table + i];
-                sh_pages[threadIdx.x] = page_or_none(id, a.cache.n_pages);
-            }
-        }
+        load_pages(a, p, sh_pages, window, stop);
         __syncthreads();
         const int* pages = sh_pages - (window >> a.cache.page_log2);
         // the keys of a wavefront's next step are on their way while it works on one; behind its last it asks for that one again
@@ -362,7 +379,7 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
         }
     }
     if (__syncthreads_or(redo)) {
-        for (int r = first_row + wave; r < min(first_row + 16 * RB, p.rows); r += 4) attend_row_alone<D, E4M3>(a, p, kh, r, lane);
+        for (int r = first_row + wave; r < min(first_row + 16 * RB, p.rows); r += 4) attend_row_alone<D, E4M3>(a, p, kh, r, lane, nullptr, 0, D);
         return;
     }
 
@@ -428,28 +445,34 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
 
 // Many rows: a workgroup's wavefronts have 32 rows each, and the keys come through LDS for all of them, kTile at a time, the next ones on their way through
 // registers meanwhile.  The products are the ones above on 32 x 32 x 16 instructions.
-constexpr int kTile = 64;
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
-// Where 16-byte chunk c of a row lies in LDS: rows of 8 (or 16 and more) chunks, 16 rows in a row's reading order never meet in a bank
+// Where 16-byte chunk c of a row lies in LDS: the same chunk of 8 rows side by side is in 8 different places of 128 bytes, of 16 rows in 16 of 256
 template <int CHUNKS>
 __device__ __forceinline__ int chunk_at(int row, int c) {
-    return row * CHUNKS + (CHUNKS == 8 ? c ^ ((row + (row >> 3)) & 7) : c ^ (row & 15));
+    return row * CHUNKS + (CHUNKS == 4 ? c ^ (((row >> 1) ^ (row >> 3)) & 3) : CHUNKS == 8 ? c ^ ((row + (row >> 3)) & 7) : c ^ (row & 15));
 }
 // The row of the K tile that key i of 32 is in: a lane's eight values of P in the order of the second product's operand (bits 2 and 3 change places)
 __device__ __forceinline__ int key_row(int i) { return (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1); }
 
+// Heads of 256 are two workgroups, of 128 of V's features each: with the sums of all 256 in registers a wavefront has its SIMD to itself, and the compiler
+// moves them about (6 pieces of up to 700 tokens, 4 key heads of 2: 244 us; with the first product made twice HALVES).
 template <int D, int NW, bool E4M3>
-__global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void attend_tiles_kernel(const AttnArgs a, const int front) {
+__global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs a, const int front) {
+    constexpr int kTile = D == 256 ? 32 : 64, kBlocks = kTile / 32;            // keys at a time, as 32 to an instruction
+    constexpr int DV = D == 256 ? 128 : D, kHalves = D / DV;
     constexpr int kThreads = 64 * NW, kCells = E4M3 ? 16 : 8;                  // of a 16-byte load
-    constexpr int kLoads = kTile * D / kCells, kEach = (kLoads + kThreads - 1) / kThreads;
+    constexpr int kLoadsK = kTile * D / kCells, kEachK = (kLoadsK + kThreads - 1) / kThreads;
+    constexpr int kLoadsV = kTile * DV / kCells, kEachV = (kLoadsV + kThreads - 1) / kThreads;
     constexpr int kRowLoads = D / kCells, kKeyLoads = kTile / kCells;          // of a key, of a feature
-    static_assert(kThreads % kRowLoads == 0 && kThreads % kKeyLoads == 0 && (kLoads % kThreads == 0 || kLoads < kThreads), "staging");
-    __shared__ u32x4_t sh_k[2][kTile * D / 8], sh_v[2][kTile * D / 8];
-    __shared__ int sh_infinite[2][NW];
+    static_assert(kThreads % kRowLoads == 0 && kThreads % kKeyLoads == 0 && (kLoadsK % kThreads == 0 || kLoadsK < kThreads) &&
+                  (kLoadsV % kThreads == 0 || kLoadsV < kThreads), "staging");
+    __shared__ u32x4_t sh_k[2][kTile * D / 8], sh_v[2][kTile * DV / 8];
+    __shared__ int sh_infinite[2][NW], sh_fewest[NW], sh_pages[kTableKeys / 16];
+    __shared__ float sh_m[32 * NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
     // key heads are the fastest index: with 8 of them, or 16 and so on, each die has heads of its own, and those in its L2
-    const int kh = blockIdx.x % a.cache.kv_heads, rest = blockIdx.x / a.cache.kv_heads;
+    const int kh = blockIdx.x % a.cache.kv_heads, rest = blockIdx.x / a.cache.kv_heads / kHalves, half = blockIdx.x / a.cache.kv_heads % kHalves;
     const int groups = ((front ? a.seqs.n_tokens : a.seqs.max_q) * a.group + 32 * NW - 1) / (32 * NW);
     const int chunk = rest / groups, first_row = (groups - 1 - rest % groups) * (32 * NW);       // the rows that see most first
     const Span p = front ? front_span(a, chunk) : own_span(a, blockIdx.y, chunk);
@@ -482,80 +505,89 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void attend_tiles_kernel
     float scale = a.scale < 0.f ? -a.scale : a.scale;
     if (E4M3 && a.cache.k_scale) scale *= as_global(a.cache.k_scale)[kh];
 
-    f32x16_t o[D / 32];
+    f32x16_t o[DV / 32];
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
+    for (int i = 0; i < DV / 32; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
     float m = kNone, l = 0.f;
     bool redo = false;
 
-    // staging: thread's key rows of K (one per load) and keys of V (the same for all its loads)
+    // staging: each thread's key rows of K (one a load), and keys of V (the same ones for all its loads, of different features)
     const int page_mask = (1 << a.cache.page_log2) - 1;
-    const int k_row = tid / kRowLoads, k_chunk = tid % kRowLoads, v_row = tid / kKeyLoads, v_key = (tid % kKeyLoads) * kCells;
-    constexpr int kRowStep = kThreads / kRowLoads, kFeatureStep = kThreads / kKeyLoads;
-    int k_page[kEach], v_page;
-    u32x4_t k_regs[kEach], v_regs[kEach];
-    int k_from[kEach], v_from;                                                 // the pages that the registers' keys are of
-    const auto page_of = [&](int key) {
-        int id = -1;
-        if (key < p.key1 && !p.bad) id = page_or_none(as_global(a.seqs.table)[p.table + (key >> a.cache.page_log2)], a.cache.n_pages);
-        return id;
-    };
-    const auto ask_pages = [&](int tile) {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) k_page[i] = page_of(tile + k_row + i * kRowStep);
-        v_page = page_of(tile + v_key);
-    };
+    const int k_row = tid / kRowLoads, v_row = tid / kKeyLoads, v_key = (tid % kKeyLoads) * kCells;
+    constexpr int kRowStep = kThreads / kRowLoads, kFeatureStep = kThreads / kKeyLoads, kBytes = 16 / kCells;
+    const uint32_t page_bytes = (uint32_t)a.cache.page_bytes;
+    const uint8_t* k_base = a.cache.k + ((((int64_t)kh * D) << a.cache.page_log2) + (tid % kRowLoads) * kCells) * kBytes;
+    const uint8_t* v_base = a.cache.v + (((int64_t)kh * D + half * DV + v_row) << a.cache.page_log2) * kBytes;
+    const uint32_t v_step = (uint32_t)(kFeatureStep * kBytes) << a.cache.page_log2;
+    u32x4_t k_regs[kEachK], v_regs[kEachV];
+    bool k_none[kEachK], v_none, any_none = false;                              // keys without a page
+    int window = p.begin, fewest_of_all = 0;
     const auto ask_keys = [&](int tile) {
-        if (kLoads < kThreads && tid >= kLoads) return;
+        const int* pages = sh_pages - (window >> a.cache.page_log2);
+        if (kLoadsK >= kThreads || tid < kLoadsK) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int key = tile + k_row + i * kRowStep;
-            k_from[i] = k_page[i];
-            k_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(a.cache.k) + max(k_page[i], 0) * a.cache.page_bytes +
-                                                                         ((((int64_t)kh << a.cache.page_log2) + (key & page_mask)) * D + k_chunk * kCells) * (16 / kCells));
+            for (int i = 0; i < kEachK; ++i) {
+                const int key = tile + k_row + i * kRowStep, page = pages[key >> a.cache.page_log2];
+                k_none[i] = page < 0;
+                k_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(k_base) + ((uint64_t)(uint32_t)max(page, 0) * page_bytes + (uint32_t)((key & page_mask) * (D * kBytes))));
+            }
         }
-        v_from = v_page;
-        const PATCH_EP_GLOBAL uint8_t* base = as_global(a.cache.v) + max(v_page, 0) * a.cache.page_bytes;
+        if (kLoadsV >= kThreads || tid < kLoadsV) {
+            const int key = tile + v_key, page = pages[key >> a.cache.page_log2];
+            v_none = page < 0;
+            const PATCH_EP_GLOBAL uint8_t* at = as_global(v_base) + ((uint64_t)(uint32_t)max(page, 0) * page_bytes + (uint32_t)((key & page_mask) * kBytes));
 #pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            v_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(base + ((((int64_t)kh * D + v_row + i * kFeatureStep) << a.cache.page_log2) + ((tile + v_key) & page_mask)) * (16 / kCells));
+            for (int i = 0; i < kEachV; ++i) v_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(at + i * v_step);
+        }
     };
     const auto put_keys = [&](int tile, int buffer) {
+        constexpr int kParts = kCells / 8;
+        const bool edge = tile < p.key0 || tile + kTile > p.key1, seen_by_all = tile + kTile <= fewest_of_all;
         bool infinite = false;
-        if (kLoads >= kThreads || tid < kLoads) {
-            const bool edge = tile < p.key0 || tile + kTile > p.key1;
+        if (kLoadsK >= kThreads || tid < kLoadsK) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const int at = k_row + i * kRowStep, row = (at & ~31) | key_row(at & 31), feature = v_row + i * kFeatureStep;
-                u32x4_t k[2], v[2];
-                if constexpr (E4M3) {
-                    k[0] = widen8(k_regs[i][0], k_regs[i][1]), k[1] = widen8(k_regs[i][2], k_regs[i][3]);
-                    v[0] = widen8(v_regs[i][0], v_regs[i][1]), v[1] = widen8(v_regs[i][2], v_regs[i][3]);
-                } else {
-                    k[0] = k_regs[i], v[0] = v_regs[i];
-                }
-                constexpr int kParts = kCells / 8;
+            for (int i = 0; i < kEachK; ++i) {
+                const int at = k_row + i * kRowStep, row = (at & ~31) | key_row(at & 31);
 #pragma unroll
                 for (int b = 0; b < kParts; ++b) {
-                    if (k_from[i] < 0) k[b] = u32x4_t{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};      // a page that is not there: NaN scores
-                    if (v_from < 0) v[b] = u32x4_t{0, 0, 0, 0};
-                    if (edge) keep_keys(v[b], tile + v_key + 8 * b, p.key0, p.key1);                             // cells that no key is in
-                    infinite |= any_infinite(v[b]);
-                    sh_k[buffer][chunk_at<D / 8>(row, k_chunk * kParts + b)] = k[b];
-                    sh_v[buffer][chunk_at<kTile / 8>(feature, v_key / 8 + b)] = v[b];
+                    u32x4_t k = k_regs[i];
+                    if constexpr (E4M3) k = widen8(k_regs[i][2 * b], k_regs[i][2 * b + 1]);
+                    if (any_none && k_none[i]) k = u32x4_t{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};     // a page that is not there: NaN scores
+                    sh_k[buffer][chunk_at<D / 8>(row, (tid % kRowLoads) * kParts + b)] = k;
                 }
             }
         }
-        infinite = __any(infinite);
-        if (lane == 0) sh_infinite[buffer][wave] = infinite;
+        if (kLoadsV >= kThreads || tid < kLoadsV) {
+#pragma unroll
+            for (int i = 0; i < kEachV; ++i) {
+#pragma unroll
+                for (int b = 0; b < kParts; ++b) {
+                    u32x4_t v = v_regs[i];
+                    if constexpr (E4M3) v = widen8(v_regs[i][2 * b], v_regs[i][2 * b + 1]);
+                    if (any_none && v_none) v = u32x4_t{0, 0, 0, 0};
+                    if (edge) keep_keys(v, tile + v_key + 8 * b, p.key0, p.key1);        // cells that no key is in
+                    if (!seen_by_all) infinite |= any_infinite(v);
+                    sh_v[buffer][chunk_at<kTile / 8>(v_row + i * kFeatureStep, v_key / 8 + b)] = v;
+                }
+            }
+        }
+        if (!seen_by_all) {
+            infinite = __any(infinite);
+            if (lane == 0) sh_infinite[buffer][wave] = infinite;
+        }
     };
 
+    if (lane == 0) sh_fewest[wave] = fewest;
+    if (p.begin < end) any_none = __syncthreads_or(load_pages(a, p, sh_pages, window, min(end, window + kTableKeys)));
+    else __syncthreads();
+    fewest_of_all = sh_fewest[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) fewest_of_all = min(fewest_of_all, sh_fewest[w]);
+    fewest_of_all = __builtin_amdgcn_readfirstlane(fewest_of_all);
     if (p.begin < end) {
-        ask_pages(p.begin);
         ask_keys(p.begin);
-        ask_pages(p.begin + kTile);
         put_keys(p.begin, 0);
         __syncthreads();
     }
@@ -563,24 +595,35 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void attend_tiles_kernel
     for (int tile = p.begin; tile < end; tile += kTile, buffer ^= 1) {
         const bool more = tile + kTile < end;
         if (more) {
+            if (tile + kTile == window + kTableKeys) {                         // (nobody looks into the table between here and the last barrier)
+                window += kTableKeys;
+                any_none = __syncthreads_or(load_pages(a, p, sh_pages, window, min(end, window + kTableKeys)));
+            }
             ask_keys(tile + kTile);
-            ask_pages(tile + 2 * kTile);
         }
         if (tile < most) {
-            f32x16_t s[2];
+            f32x16_t s[kBlocks];
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < kBlocks; ++b)
                     s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh_k[buffer][chunk_at<D / 8>(32 * b + col, 2 * i + h)]), q[i], s[b], 0, 0, 0);
+            // the operands of the next few products are on their way out of LDS while one runs
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+            for (int i = 0; i < kBlocks * D / 16 - 6; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
             const bool ragged = tile < p.key0 || tile + kTile > fewest;
             if (ragged) {
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int key = tile + 32 * b + 16 * (e / 8) + 8 * h + e % 8;
@@ -589,7 +632,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void attend_tiles_kernel
             }
             float top = s[0][0];
 #pragma unroll
-            for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
+            for (int e = 1; e < kTile / 2; ++e) top = fmaxf(top, s[e / 16][e % 16]);
             top = top == kNone ? kNone : top * scale;                          // (a scale of zero makes no NaN of it)
             if (__any(top > m + kRise)) {
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -597,30 +640,30 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void attend_tiles_kernel
                 m = m_new;
                 l *= down;
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) o[i] = o[i] * down;
+                for (int i = 0; i < DV / 32; ++i) o[i] = o[i] * down;
             }
             const float off = m == kNone ? 0.f : m;
-            bf16x8_t pr[4];
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            bf16x8_t pr[kTile / 16];
+            float sum[2] = {0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < kTile / 16; ++k) {
                 float y[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 2][8 * (k % 2) + e], scale, -off));
-                    sum[k] += y[e];
+                    sum[k % 2] += y[e];
                 }
                 pr[k] = as_bf16x8(u32x4_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])});
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            if (ragged && fewest < min(tile + kTile, p.key1)) {                // keys that only some of the rows see, and not finite?
+            l += sum[0] + sum[1];
+            if (fewest < min(tile + kTile, p.key1)) {                          // keys that only some of the rows see, and not finite?
 #pragma unroll
                 for (int w = 0; w < NW; ++w) redo |= sh_infinite[buffer][w] != 0;
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < kTile / 16; ++k)
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i)
+                for (int i = 0; i < DV / 32; ++i)
                     o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh_v[buffer][chunk_at<kTile / 8>(32 * i + col, 2 * k + h)]), pr[k], o[i], 0, 0, 0);
         }
         if (more) put_keys(tile + kTile, buffer ^ 1);
@@ -628,7 +671,9 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void attend_tiles_kernel
     }
 
     if (__syncthreads_or(redo)) {
-        for (int r1 = first_row + wave; r1 < min(first_row + 32 * NW, p.rows); r1 += NW) attend_row_alone<D, E4M3>(a, p, kh, r1, lane);
+        if (h == 0) sh_m[32 * wave + col] = m;
+        __syncthreads();
+        for (int i = wave; i < min(32 * NW, p.rows - first_row); i += NW) attend_row_alone<D, E4M3>(a, p, kh, first_row + i, lane, &sh_m[i], half * DV, DV);
         return;
     }
     l += __shfl_xor(l, 32);
@@ -640,23 +685,23 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void attend_tiles_kernel
     const int64_t row = token * a.heads + head;
     if (p.part < 0) {
         const float over = (l == 0.f ? 0.f : 1.f / l) * v_scale;
-        const int64_t at = token * a.o_stride + (int64_t)head * D + 4 * h;
+        const int64_t at = token * a.o_stride + (int64_t)head * D + half * DV + 4 * h;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
+        for (int i = 0; i < DV / 32; ++i)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
                 *reinterpret_cast<PATCH_EP_GLOBAL u32x2_t*>(as_global_out(a.O) + at + 32 * i + 2 * e) =
                     u32x2_t{bf16_pair(o[i][e] * over, o[i][e + 1] * over), bf16_pair(o[i][e + 2] * over, o[i][e + 3] * over)};
-        if (a.lse && h == 0) as_global_out(a.lse)[row] = 0.6931471805599453f * (m + __builtin_log2f(l));
+        if (a.lse && h == 0 && half == 0) as_global_out(a.lse)[row] = 0.6931471805599453f * (m + __builtin_log2f(l));
     } else {
         const int64_t at = (int64_t)p.part * a.seqs.n_tokens * a.heads + row;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
+        for (int i = 0; i < DV / 32; ++i)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<PATCH_EP_GLOBAL f32x4_t*>(as_global_out(a.part_o) + at * D + 4 * h + 32 * i + 2 * e) =
+                *reinterpret_cast<PATCH_EP_GLOBAL f32x4_t*>(as_global_out(a.part_o) + at * D + half * DV + 4 * h + 32 * i + 2 * e) =
                     f32x4_t{o[i][e] * v_scale, o[i][e + 1] * v_scale, o[i][e + 2] * v_scale, o[i][e + 3] * v_scale};
-        if (h == 0) {
+        if (h == 0 && half == 0) {
             as_global_out(a.part_ml)[2 * at] = m;
             as_global_out(a.part_ml)[2 * at + 1] = l;
         }
@@ -715,7 +760,9 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const AttnArgs a) {
 static int rows_of_block(int64_t rows, int head_dim) {
     if (rows <= 16) return 16;
     if (rows <= 32 && head_dim <= 128) return 32;
-    return rows <= 128 || head_dim == 256 ? 128 : 256;
+    
+    return rows <= 128 ? 128 : 256;
+
 }
 
 // Keys that a workgroup takes, so that a launch over `keys` of them for `units` sequences, key heads and blocks of rows is two workgroups of four wavefronts
@@ -741,20 +788,23 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     a->prefix_parts = 0;
     a->parts = 1;
     if (a->prefix > a->seqs.max_kv) a->prefix = a->seqs.max_kv;
-    if (most < 2 || a->seqs.n_seqs < 2) a->prefix = 0;        // every sequence reads the shared keys as its own
     const auto blocks = [&](int64_t tokens, int block) { return (tokens * a->group + block - 1) / block; };
+    const int block = rows_of_block((int64_t)a->seqs.max_q * a->group, D);
+    const int64_t units = blocks(a->seqs.max_q, block) * heads;
+    // Every sequence reads the shared keys as its own where it has to, and where blocks of 128 rows and more, for which reading keys is little of the work, fill
+    // the chip without being cut: 32 pieces of 64 tokens, 8 key heads of 4 query heads, behind 2048 shared keys 100 us so, 211 in parts; 6 pieces of 200
+    // tokens (192 workgroups) 130 and 109, 8 of 70 behind 8192 (128) 176 and 133.
+    if (most < 2 || a->seqs.n_seqs < 2 || (block >= 128 && units * a->seqs.n_seqs >= 256)) a->prefix = 0;
     int64_t prefix_parts = 0;
     if (a->prefix) {
-        const int block = rows_of_block((int64_t)a->seqs.n_tokens * a->group, D);
-        const int64_t units = blocks(a->seqs.n_tokens, block) * heads;
-        int64_t chunk = chunk_of(a->prefix, units, block, units);
+        const int front = rows_of_block((int64_t)a->seqs.n_tokens * a->group, D);
+        const int64_t front_units = blocks(a->seqs.n_tokens, front) * heads;
+        int64_t chunk = chunk_of(a->prefix, front_units, front, front_units);
         if ((a->prefix + chunk - 1) / chunk > most / 2) chunk = up_to((a->prefix + most / 2 - 1) / (most / 2), 128);
         a->prefix_chunk = (int)chunk;
         prefix_parts = (a->prefix + chunk - 1) / chunk;
     }
     const int64_t own = a->seqs.max_kv - (a->prefix & ~31), left = most - prefix_parts;
-    const int block = rows_of_block((int64_t)a->seqs.max_q * a->group, D);
-    const int64_t units = blocks(a->seqs.max_q, block) * heads;
     int64_t chunk = chunk_of(own, units * a->seqs.n_seqs, block, units);
     if (left < 2 && !a->prefix) chunk = up_to(own > 0 ? own : 1, 128);
     else if ((own + chunk - 1) / chunk > left) chunk = up_to((own + left - 1) / left, 128);
@@ -778,7 +828,7 @@ template <int D, int NW, bool E4M3>
 static void launch_tiles(const AttnArgs& a, int front, hipStream_t stream) {
     const int tokens = front ? a.seqs.n_tokens : a.seqs.max_q, parts = front ? a.prefix_parts : a.parts - a.prefix_parts;
     const unsigned groups = (unsigned)(((int64_t)tokens * a.group + 32 * NW - 1) / (32 * NW));
-    attend_tiles_kernel<D, NW, E4M3><<<dim3(parts * groups * (unsigned)a.cache.kv_heads, front ? 1u : (unsigned)a.seqs.n_seqs), 64 * NW, 0, stream>>>(a, front);
+    attend_tiles_kernel<D, NW, E4M3><<<dim3(parts * groups * (unsigned)a.cache.kv_heads * (D == 256 ? 2u : 1u), front ? 1u : (unsigned)a.seqs.n_seqs), 64 * NW, 0, stream>>>(a, front);
 }
 
 template <int D, bool E4M3>
@@ -788,7 +838,7 @@ static void launch_rows_of(const AttnArgs& a, hipStream_t stream) {
         if (block == 16) launch_rows<D, 1, E4M3>(a, front, stream);
         else if (block == 32) launch_rows<D, D == 256 ? 1 : 2, E4M3>(a, front, stream);
         else if (block == 128) launch_tiles<D, 4, E4M3>(a, front, stream);
-        else launch_tiles<D, D == 256 ? 4 : 8, E4M3>(a, front, stream);
+        else launch_tiles<D, 8, E4M3>(a, front, stream);
     }
 }
 

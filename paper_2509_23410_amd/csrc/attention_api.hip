@@ -66,6 +66,7 @@ static patch_status fill_cache(CacheArgs* to, const patch_kv_cache* c) {
     to->k = static_cast<uint8_t*>(c->k);
     to->v = static_cast<uint8_t*>(c->v);
     to->page_bytes = (c->page_stride ? c->page_stride : cells) * (c->e4m3 ? 1 : 2);
+    if (to->page_bytes >= ((int64_t)1 << 32)) return PATCH_ERR_SHAPE;
     to->k_scale = c->k_scale;
     to->v_scale = c->v_scale;
     to->n_pages = (int)c->n_pages;
@@ -180,6 +181,7 @@ patch_status patch_attention(const void* Q, int64_t q_stride, int heads, const p
     a.o_stride = o_stride;
     a.scale = scale * 1.4426950408889634f;
     if (seqs->n_tokens == 0 || seqs->max_q == 0) return PATCH_OK;
+    if (Q == O) return PATCH_ERR_ARG;
     plan_attention(&a, ws_bytes);
     launch_attention(a, static_cast<hipStream_t>(stream));
     return launched();
