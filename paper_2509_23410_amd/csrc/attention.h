@@ -40,6 +40,7 @@ struct RopeArgs {
     CacheArgs cache;          // k null: no cache, K goes to k.out
     int64_t n_tokens, n_pos;
     int head_dim, rot, interleaved, f32;
+    int v_tiles;              // filled in by launch_rope
     float eps;
 };
 void launch_rope(const RopeArgs& a, hipStream_t stream);

@@ -456,7 +456,7 @@ __device__ __forceinline__ int chunk_at(int row, int c) {
 __device__ __forceinline__ int key_row(int i) { return (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1); }
 
 // Heads of 256 are two workgroups, of 128 of V's features each: with the sums of all 256 in registers a wavefront has its SIMD to itself, and the compiler
-// moves them about (6 pieces of up to 700 tokens, 4 key heads of 2: 244 us; with the first product made twice HALVES).
+// moves them about (6 pieces of up to 700 tokens, 4 key heads of 2: 244 us, and 127 so, though the first product is made twice).
 template <int D, int NW, bool E4M3>
 __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs a, const int front) {
     constexpr int kTile = D == 256 ? 32 : 64, kBlocks = kTile / 32;            // keys at a time, as 32 to an instruction
@@ -790,7 +790,8 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     if (a->prefix > a->seqs.max_kv) a->prefix = a->seqs.max_kv;
     const auto blocks = [&](int64_t tokens, int block) { return (tokens * a->group + block - 1) / block; };
     const int block = rows_of_block((int64_t)a->seqs.max_q * a->group, D);
-    const int64_t units = blocks(a->seqs.max_q, block) * heads;
+    const auto halves = [&](int block) { return D == 256 && block >= 128 ? 2 : 1; };      // workgroups of such a block
+    const int64_t units = blocks(a->seqs.max_q, block) * heads * halves(block);
     // Every sequence reads the shared keys as its own where it has to, and where blocks of 128 rows and more, for which reading keys is little of the work, fill
     // the chip without being cut: 32 pieces of 64 tokens, 8 key heads of 4 query heads, behind 2048 shared keys 100 us so, 211 in parts; 6 pieces of 200
     // tokens (192 workgroups) 130 and 109, 8 of 70 behind 8192 (128) 176 and 133.
@@ -798,7 +799,7 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     int64_t prefix_parts = 0;
     if (a->prefix) {
         const int front = rows_of_block((int64_t)a->seqs.n_tokens * a->group, D);
-        const int64_t front_units = blocks(a->seqs.n_tokens, front) * heads;
+        const int64_t front_units = blocks(a->seqs.n_tokens, front) * heads * halves(front);
         int64_t chunk = chunk_of(a->prefix, front_units, front, front_units);
         if ((a->prefix + chunk - 1) / chunk > most / 2) chunk = up_to((a->prefix + most / 2 - 1) / (most / 2), 128);
         a->prefix_chunk = (int)chunk;

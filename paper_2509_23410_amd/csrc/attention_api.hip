@@ -22,7 +22,7 @@ static patch_status launched() {
 
 // writes: the call writes h->out
 static patch_status fill_heads(HeadArgs* to, const patch_heads* h, int head_dim, int f32, bool writes) {
-    if (!h->x || h->heads < 1 || h->heads > (1 << 16) || (h->f32 != 0) != (f32 != 0)) return PATCH_ERR_ARG;
+    if (!h->x || h->heads < 1 || h->heads > 16384 || (h->f32 != 0) != (f32 != 0)) return PATCH_ERR_ARG;
     const int size = f32 ? 4 : 2;
     if (!aligned(h->x) || !aligned(h->gamma)) return PATCH_ERR_ARG;
     const int64_t width = (int64_t)h->heads * head_dim;

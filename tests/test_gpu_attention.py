@@ -89,7 +89,12 @@ APPENDS = [
     ([1], [1], 2, 64, 16, 0, False, 14, True, True, 64, False, 0), ([1, 1, 1], [17, 16, 5], 8, 128, 64, 0, False, 0, False, False, 0, False, 64),
     ([1] * 5, [100, 33, 1, 64, 65], 3, 128, 32, 33, True, 6, True, True, 128, False, 0), ([5, 0, 3, 70], [5, 40, 130, 70], 2, 128, 16, 0, False, 4, False, True, 64, True, 16),
     ([40, 129, 1], [300, 129, 1], 2, 256, 128, 0, True, 2, True, False, 256, True, 32), ([3, 2, 4], [2, 0, 9], 2, 64, 256, 0, False, 2, True, True, 16, False, 0),
-    ([200], [1000], 5, 64, 64, 512, True, 0, False, False, 64, False, 0), ([17, 64, 63], [80, 64, 127], 1, 128, 16, 0, True, 1, False, True, 8, False, 0)]
+    ([200], [1000], 5, 64, 64, 512, True, 0, False, False, 64, False, 0), ([17, 64, 63], [80, 64, 127], 1, 128, 16, 0, True, 1, False, True, 8, False, 0),
+    # enough tokens for tiles of V, and (the last two) for several heads a thread
+    ([300, 7, 64], [411, 7, 64], 2, 64, 16, 0, False, 3, True, True, 64, False, 0), ([130, 200], [100, 333], 3, 128, 32, 0, True, 0, False, False, 0, False, 32),
+    ([256], [256], 1, 256, 256, 0, False, 4, False, True, 256, True, 0), ([65, 300, 1], [200, 300, 40], 2, 256, 64, 0, True, 0, True, False, 64, False, 0),
+    ([9] * 40, [100 + 3 * i for i in range(40)], 2, 64, 128, 64, False, 0, False, False, 64, False, 16), ([1100], [1203], 7, 256, 128, 0, False, 12, True, True, 128, False, 0),
+    ([600, 450], [600, 777], 9, 128, 64, 0, True, 24, False, True, 128, True, 0)]
 
 
 @pytest.mark.parametrize("n,kv,KH,D,page,prefix,e4m3,H,f32,norm,rot,interleaved,gap", APPENDS)
