@@ -483,7 +483,7 @@ typedef struct {
  * The numbers on the device are not read by the host.  Page numbers outside 0 .. n_pages - 1, and lengths beyond max_kv or
  * the table, are not followed: patch_kv_append writes nothing there, and the rows of patch_attention that need them are NaN. */
 typedef struct {
-    int64_t n_seqs;             /* 1 .. 65535                                                                                    */
+    int64_t n_seqs;             /* 1 .. 65535; times kv_heads at most 2^22 in patch_attention                                    */
     int64_t n_tokens;           /* rows of the call: up to 2^23, and up to 2^25 heads of them in patch_attention                 */
     const int32_t* q_start;     /* DEVICE, n_seqs + 1, never falling; NULL: one token each (n_tokens == n_seqs)                  */
     const int32_t* kv_len;      /* DEVICE, n_seqs: with the new tokens                                                           */

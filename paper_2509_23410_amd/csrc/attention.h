@@ -57,11 +57,15 @@ struct AttnArgs {
     int prefix;               // keys [0, prefix) are those of the first sequence's row for all; they take parts of their own
     int own_chunk;            // keys of a sequence's own that one workgroup takes: a multiple of 128, counted from prefix rounded down to 32
     int prefix_chunk, prefix_parts;
-    int parts;                // prefix_parts + the own chunks of max_kv keys; 1: workgroups write O, else partial results
+    int parts;                // prefix_parts + the most that a sequence's own keys are; 1: workgroups write O, else partial results
+    // few rows a sequence: one launch of front_blocks workgroups for the shared front and own_blocks that have equal stretches (least_blocks at least) of all
+    // own keys, in blocks of block_keys; 0: a workgroup for each sequence and key head
+    int few, front_blocks, own_blocks, block_keys, least_blocks;
     float* part_ml;           // parts x n_tokens x heads pairs: running maximum (of scores times log2(e)) and sum
     float* part_o;            // parts x n_tokens x heads x head_dim
+    int* unit_parts;          // n_seqs x kv_heads: the parts of its own keys
 };
-// fills own_chunk, prefix_chunk, prefix_parts and parts for a workspace of ws_bytes (0: none), prefix too where it does without; returns the bytes used
+// fills all that from own_chunk on for a workspace of ws_bytes (0: none), prefix too where it does without; returns the bytes used
 size_t plan_attention(AttnArgs* a, size_t ws_bytes);
 void launch_attention(const AttnArgs& a, hipStream_t stream);
 

@@ -10,6 +10,7 @@
 // both, and the second product's B operand is what the lane already holds of the first's result, if the keys of a step are given out to the rows of A
 // in the right order: no value of P crosses lanes.  V lies feature-major in its pages, so V^T's operand is a plain 16-byte load too.
 #include <algorithm>
+#include <type_traits>
 
 #include "cells.h"
 
@@ -67,8 +68,7 @@ __device__ __forceinline__ int own_parts(const AttnArgs& a, int len) {
     return len > a.prefix ? (len - base + a.own_chunk - 1) / a.own_chunk : 0;
 }
 
-__device__ __forceinline__ Span own_span(const AttnArgs& a, int s, int chunk) {
-    const Seq q = seq_at(a.seqs, s);
+__device__ __forceinline__ Span own_span(const AttnArgs& a, int s, const Seq& q, int chunk) {
     Span p;
     p.front = false;
     p.t0 = q.first;
@@ -77,7 +77,7 @@ __device__ __forceinline__ Span own_span(const AttnArgs& a, int s, int chunk) {
     p.key0 = a.prefix;
     p.key1 = max(q.len, a.prefix);
     p.begin = (a.prefix & ~31) + chunk * a.own_chunk;
-    p.end = min(q.len, p.begin + a.own_chunk);
+    p.end = a.block_keys ? q.len : min(q.len, p.begin + a.own_chunk);
     p.part = a.parts == 1 || (a.prefix_parts == 0 && q.len - p.begin <= a.own_chunk && chunk == 0) ? -1 : a.prefix_parts + chunk;
     p.table = s * a.seqs.table_stride;
     p.bad = q.bad;
@@ -242,23 +242,21 @@ __device__ __forceinline__ bf16x8_t key_operand(const KeyRegs<D, E4M3>& r, int b
 template <bool E4M3>
 __device__ __forceinline__ int query_offset(int i, int g) { return E4M3 ? 64 * (i / 2) + 16 * g + 8 * (i % 2) : 32 * i + 8 * g; }
 
-template <int D, int RB, bool E4M3>
-__global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel(const AttnArgs a, const int front) {
-    constexpr int kPitch = D + 4;
-    __shared__ float sh_o[4][16][kPitch];
-    __shared__ float sh_m[4][RB * 16], sh_l[4][RB * 16];
-    __shared__ int sh_pages[kTableKeys / 16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
-    const int kh = blockIdx.y, groups = ((front ? a.seqs.n_tokens : a.seqs.max_q) * a.group + 16 * RB - 1) / (16 * RB);
-    const int first_row = (blockIdx.x % groups) * (16 * RB), chunk = blockIdx.x / groups;
-    const Span p = front ? front_span(a, chunk) : own_span(a, blockIdx.z, chunk);
-    if (first_row >= p.rows) return;
-    if (p.begin >= p.end && (p.part >= 0 || chunk > 0)) return;     // no keys here; the first workgroup of rows that see none writes that
+template <int D, int RB>
+struct RowsLds {
+    float o[4][16][D + 4], m[4][RB * 16], l[4][RB * 16];
+    int pages[kTableKeys / 16];
+};
 
+// All rows of a span (16 RB at most), by a workgroup of four wavefronts.
+template <int D, int RB, bool E4M3>
+__device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, int kh, RowsLds<D, RB>& sh) {
+    constexpr bool kAhead = D * RB <= 128;      // with more, two steps' keys do not fit beside the rest in half a SIMD's registers
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
     int limit[RB], fewest = 0x7FFFFFFF, most = 0;
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        const int r = first_row + 16 * b + col;
+        const int r = 16 * b + col;
         limit[b] = row_limit(a, p, r);
         if (r < p.rows) fewest = min(fewest, limit[b]);
         most = max(most, limit[b]);
@@ -274,7 +272,7 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
     bf16x8_t q[RB][D / 32];
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        const int r = first_row + 16 * b + col;
+        const int r = 16 * b + col;
         const bool there = r < p.rows;
         const int64_t at = there ? (int64_t)(p.t0 + r / a.group) * a.q_stride + (int64_t)(kh * a.group + r % a.group) * D : 0;
 #pragma unroll
@@ -302,16 +300,17 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
         const int stop = min(end, window + kTableKeys);
         // page numbers, as steps of 32 keys may touch them: -1 where there is none or it is out of range
         if (window != p.begin) __syncthreads();
-        load_pages(a, p, sh_pages, window, stop);
+        load_pages(a, p, sh.pages, window, stop);
         __syncthreads();
-        const int* pages = sh_pages - (window >> a.cache.page_log2);
+        const int* pages = sh.pages - (window >> a.cache.page_log2);
         // the keys of a wavefront's next step are on their way while it works on one; behind its last it asks for that one again
         KeyRegs<D, E4M3> next;
         const int first_step = window + 32 * wave, last_step = first_step + (max(stop - 1 - first_step, 0) & ~127);
-        if (first_step < stop) load_keys<D, E4M3>(next, a, pages, first_step, kh, lane);
+        if (kAhead && first_step < stop) load_keys<D, E4M3>(next, a, pages, first_step, kh, lane);
         for (int step = first_step; step < stop; step += 128) {
-            const KeyRegs<D, E4M3> kv = next;
-            load_keys<D, E4M3>(next, a, pages, min(step + 128, last_step), kh, lane);
+            KeyRegs<D, E4M3> kv = next;
+            if constexpr (kAhead) load_keys<D, E4M3>(next, a, pages, min(step + 128, last_step), kh, lane);
+            else load_keys<D, E4M3>(kv, a, pages, step, kh, lane);
             f32x4_t s[RB][2];
 #pragma unroll
             for (int b = 0; b < RB; ++b) s[b][0] = s[b][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -379,7 +378,7 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
         }
     }
     if (__syncthreads_or(redo)) {
-        for (int r = first_row + wave; r < min(first_row + 16 * RB, p.rows); r += 4) attend_row_alone<D, E4M3>(a, p, kh, r, lane, nullptr, 0, D);
+        for (int r = wave; r < min(16 * RB, p.rows); r += 4) attend_row_alone<D, E4M3>(a, p, kh, r, lane, nullptr, 0, D);
         return;
     }
 
@@ -389,8 +388,8 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
         l[b] += __shfl_xor(l[b], 16);
         l[b] += __shfl_xor(l[b], 32);
         if (g == 0) {
-            sh_m[wave][16 * b + col] = m[b];
-            sh_l[wave][16 * b + col] = l[b];
+            sh.m[wave][16 * b + col] = m[b];
+            sh.l[wave][16 * b + col] = l[b];
         }
     }
     float v_scale = 1.f;
@@ -400,18 +399,18 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
         __syncthreads();
         float top = kNone;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, sh_m[w][16 * b + col]);
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, sh.m[w][16 * b + col]);
         const float down = exp2_off(m[b], top);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4_t*>(&sh_o[wave][col][16 * i + 4 * g]) = o[b][i] * down;
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4_t*>(&sh.o[wave][col][16 * i + 4 * g]) = o[b][i] * down;
         __syncthreads();
-        const int c = threadIdx.x / 16, d0 = (threadIdx.x % 16) * (D / 16), r = first_row + 16 * b + c;
+        const int c = threadIdx.x / 16, d0 = (threadIdx.x % 16) * (D / 16), r = 16 * b + c;
         if (r < p.rows) {
             float mc = kNone, lc = 0.f;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) mc = fmaxf(mc, sh_m[w][16 * b + c]);
+            for (int w = 0; w < 4; ++w) mc = fmaxf(mc, sh.m[w][16 * b + c]);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) lc += sh_l[w][16 * b + c] * exp2_off(sh_m[w][16 * b + c], mc);
+            for (int w = 0; w < 4; ++w) lc += sh.l[w][16 * b + c] * exp2_off(sh.m[w][16 * b + c], mc);
             const int64_t row = (int64_t)(p.t0 + r / a.group) * a.heads + kh * a.group + r % a.group;
             // p.part < 0: the result itself, over its sum (0 where the row sees nothing)
             const float over = (p.part < 0 ? (lc == 0.f ? 0.f : 1.f / lc) : 1.f) * v_scale;
@@ -420,7 +419,7 @@ __global__ __launch_bounds__(256, D * RB <= 128 ? 2 : 1) void attend_rows_kernel
             for (int i = 0; i < D / 64; ++i) {
                 out[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int w = 0; w < 4; ++w) out[i] += *reinterpret_cast<const f32x4_t*>(&sh_o[w][c][d0 + 4 * i]);
+                for (int w = 0; w < 4; ++w) out[i] += *reinterpret_cast<const f32x4_t*>(&sh.o[w][c][d0 + 4 * i]);
                 out[i] *= over;
             }
             if (p.part < 0) {
@@ -457,28 +456,26 @@ __device__ __forceinline__ int key_row(int i) { return (i & ~12) | ((i & 4) << 1
 
 // Heads of 256 are two workgroups, of 128 of V's features each: with the sums of all 256 in registers a wavefront has its SIMD to itself, and the compiler
 // moves them about (6 pieces of up to 700 tokens, 4 key heads of 2: 244 us, and 127 so, though the first product is made twice).
+template <int D, int NW>
+struct TilesLds {
+    static constexpr int kTile = D == 256 ? 32 : 64, DV = D == 256 ? 128 : D;
+    u32x4_t k[2][kTile * D / 8], v[2][kTile * DV / 8];
+    int infinite[2][NW], fewest[NW], pages[kTableKeys / 16];
+    float m[32 * NW];
+};
+
+// 32 NW rows of a span from first_row on, by a workgroup of NW wavefronts.
 template <int D, int NW, bool E4M3>
-__global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs a, const int front) {
-    constexpr int kTile = D == 256 ? 32 : 64, kBlocks = kTile / 32;            // keys at a time, as 32 to an instruction
-    constexpr int DV = D == 256 ? 128 : D, kHalves = D / DV;
+__device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, int kh, int half, int first_row, TilesLds<D, NW>& sh) {
+    constexpr int kTile = TilesLds<D, NW>::kTile, kBlocks = kTile / 32;        // keys at a time, as 32 to an instruction
+    constexpr int DV = TilesLds<D, NW>::DV;
     constexpr int kThreads = 64 * NW, kCells = E4M3 ? 16 : 8;                  // of a 16-byte load
     constexpr int kLoadsK = kTile * D / kCells, kEachK = (kLoadsK + kThreads - 1) / kThreads;
     constexpr int kLoadsV = kTile * DV / kCells, kEachV = (kLoadsV + kThreads - 1) / kThreads;
     constexpr int kRowLoads = D / kCells, kKeyLoads = kTile / kCells;          // of a key, of a feature
     static_assert(kThreads % kRowLoads == 0 && kThreads % kKeyLoads == 0 && (kLoadsK % kThreads == 0 || kLoadsK < kThreads) &&
                   (kLoadsV % kThreads == 0 || kLoadsV < kThreads), "staging");
-    __shared__ u32x4_t sh_k[2][kTile * D / 8], sh_v[2][kTile * DV / 8];
-    __shared__ int sh_infinite[2][NW], sh_fewest[NW], sh_pages[kTableKeys / 16];
-    __shared__ float sh_m[32 * NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
-    // key heads are the fastest index: with 8 of them, or 16 and so on, each die has heads of its own, and those in its L2
-    const int kh = blockIdx.x % a.cache.kv_heads, rest = blockIdx.x / a.cache.kv_heads / kHalves, half = blockIdx.x / a.cache.kv_heads % kHalves;
-    const int groups = ((front ? a.seqs.n_tokens : a.seqs.max_q) * a.group + 32 * NW - 1) / (32 * NW);
-    const int chunk = rest / groups, first_row = (groups - 1 - rest % groups) * (32 * NW);       // the rows that see most first
-    const Span p = front ? front_span(a, chunk) : own_span(a, blockIdx.y, chunk);
-    if (first_row >= p.rows) return;
-    if (p.begin >= p.end && (p.part >= 0 || chunk > 0)) return;
-
     const int r = first_row + 32 * wave + col;
     const bool there = r < p.rows;
     const int limit = row_limit(a, p, r);
@@ -491,7 +488,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs
     fewest = __builtin_amdgcn_readfirstlane(fewest);
     most = __builtin_amdgcn_readfirstlane(most);
     // keys up to the last one that any row of the workgroup sees
-    const int end = front ? p.end : min(p.end, p.pos0 + min(first_row + 32 * NW - 1, p.rows - 1) / a.group + 1);
+    const int end = p.front ? p.end : min(p.end, p.pos0 + min(first_row + 32 * NW - 1, p.rows - 1) / a.group + 1);
 
     const int64_t q_at = there ? (int64_t)(p.t0 + r / a.group) * a.q_stride + (int64_t)(kh * a.group + r % a.group) * D : 0;
     bf16x8_t q[D / 16];
@@ -525,7 +522,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs
     bool k_none[kEachK], v_none, any_none = false;                              // keys without a page
     int window = p.begin, fewest_of_all = 0;
     const auto ask_keys = [&](int tile) {
-        const int* pages = sh_pages - (window >> a.cache.page_log2);
+        const int* pages = sh.pages - (window >> a.cache.page_log2);
         if (kLoadsK >= kThreads || tid < kLoadsK) {
 #pragma unroll
             for (int i = 0; i < kEachK; ++i) {
@@ -555,7 +552,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs
                     u32x4_t k = k_regs[i];
                     if constexpr (E4M3) k = widen8(k_regs[i][2 * b], k_regs[i][2 * b + 1]);
                     if (any_none && k_none[i]) k = u32x4_t{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};     // a page that is not there: NaN scores
-                    sh_k[buffer][chunk_at<D / 8>(row, (tid % kRowLoads) * kParts + b)] = k;
+                    sh.k[buffer][chunk_at<D / 8>(row, (tid % kRowLoads) * kParts + b)] = k;
                 }
             }
         }
@@ -569,22 +566,22 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs
                     if (any_none && v_none) v = u32x4_t{0, 0, 0, 0};
                     if (edge) keep_keys(v, tile + v_key + 8 * b, p.key0, p.key1);        // cells that no key is in
                     if (!seen_by_all) infinite |= any_infinite(v);
-                    sh_v[buffer][chunk_at<kTile / 8>(v_row + i * kFeatureStep, v_key / 8 + b)] = v;
+                    sh.v[buffer][chunk_at<kTile / 8>(v_row + i * kFeatureStep, v_key / 8 + b)] = v;
                 }
             }
         }
         if (!seen_by_all) {
             infinite = __any(infinite);
-            if (lane == 0) sh_infinite[buffer][wave] = infinite;
+            if (lane == 0) sh.infinite[buffer][wave] = infinite;
         }
     };
 
-    if (lane == 0) sh_fewest[wave] = fewest;
-    if (p.begin < end) any_none = __syncthreads_or(load_pages(a, p, sh_pages, window, min(end, window + kTableKeys)));
+    if (lane == 0) sh.fewest[wave] = fewest;
+    if (p.begin < end) any_none = __syncthreads_or(load_pages(a, p, sh.pages, window, min(end, window + kTableKeys)));
     else __syncthreads();
-    fewest_of_all = sh_fewest[0];
+    fewest_of_all = sh.fewest[0];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) fewest_of_all = min(fewest_of_all, sh_fewest[w]);
+    for (int w = 1; w < NW; ++w) fewest_of_all = min(fewest_of_all, sh.fewest[w]);
     fewest_of_all = __builtin_amdgcn_readfirstlane(fewest_of_all);
     if (p.begin < end) {
         ask_keys(p.begin);
@@ -597,7 +594,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs
         if (more) {
             if (tile + kTile == window + kTableKeys) {                         // (nobody looks into the table between here and the last barrier)
                 window += kTableKeys;
-                any_none = __syncthreads_or(load_pages(a, p, sh_pages, window, min(end, window + kTableKeys)));
+                any_none = __syncthreads_or(load_pages(a, p, sh.pages, window, min(end, window + kTableKeys)));
             }
             ask_keys(tile + kTile);
         }
@@ -611,7 +608,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
-                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh_k[buffer][chunk_at<D / 8>(32 * b + col, 2 * i + h)]), q[i], s[b], 0, 0, 0);
+                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh.k[buffer][chunk_at<D / 8>(32 * b + col, 2 * i + h)]), q[i], s[b], 0, 0, 0);
             // the operands of the next few products are on their way out of LDS while one runs
             __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
@@ -658,22 +655,22 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs
             l += sum[0] + sum[1];
             if (fewest < min(tile + kTile, p.key1)) {                          // keys that only some of the rows see, and not finite?
 #pragma unroll
-                for (int w = 0; w < NW; ++w) redo |= sh_infinite[buffer][w] != 0;
+                for (int w = 0; w < NW; ++w) redo |= sh.infinite[buffer][w] != 0;
             }
 #pragma unroll
             for (int k = 0; k < kTile / 16; ++k)
 #pragma unroll
                 for (int i = 0; i < DV / 32; ++i)
-                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh_v[buffer][chunk_at<kTile / 8>(32 * i + col, 2 * k + h)]), pr[k], o[i], 0, 0, 0);
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh.v[buffer][chunk_at<kTile / 8>(32 * i + col, 2 * k + h)]), pr[k], o[i], 0, 0, 0);
         }
         if (more) put_keys(tile + kTile, buffer ^ 1);
         __syncthreads();
     }
 
     if (__syncthreads_or(redo)) {
-        if (h == 0) sh_m[32 * wave + col] = m;
+        if (h == 0) sh.m[32 * wave + col] = m;
         __syncthreads();
-        for (int i = wave; i < min(32 * NW, p.rows - first_row); i += NW) attend_row_alone<D, E4M3>(a, p, kh, first_row + i, lane, &sh_m[i], half * DV, DV);
+        for (int i = wave; i < min(32 * NW, p.rows - first_row); i += NW) attend_row_alone<D, E4M3>(a, p, kh, first_row + i, lane, &sh.m[i], half * DV, DV);
         return;
     }
     l += __shfl_xor(l, 32);
@@ -708,6 +705,118 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs
     }
 }
 
+template <int D, int NW, bool E4M3>
+__global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs a, const int front) {
+    __shared__ TilesLds<D, NW> sh;
+    constexpr int kHalves = D / TilesLds<D, NW>::DV;
+    // key heads are the fastest index: with 8 of them, or 16 and so on, each die has heads of its own, and those in its L2
+    const int kh = blockIdx.x % a.cache.kv_heads, rest = blockIdx.x / a.cache.kv_heads / kHalves, half = blockIdx.x / a.cache.kv_heads % kHalves;
+    const int groups = ((front ? a.seqs.n_tokens : a.seqs.max_q) * a.group + 32 * NW - 1) / (32 * NW);
+    const int chunk = rest / groups, first_row = (groups - 1 - rest % groups) * (32 * NW);       // the rows that see most first
+    const Span p = front ? front_span(a, chunk) : own_span(a, blockIdx.y, seq_at(a.seqs, blockIdx.y), chunk);
+    if (first_row >= p.rows) return;
+    if (p.begin >= p.end && (p.part >= 0 || chunk > 0)) return;                // no keys here; the first workgroup of rows that see none writes that
+    attend_tiles<D, NW, E4M3>(a, p, kh, half, first_row, sh);
+}
+
+// Few rows a sequence: the first front_blocks workgroups have the shared front, for all rows (in blocks of 128); beside them, on the same compute units, the
+// others have the sequences' own keys.  Those are one line, sequence by sequence and head by head in it, in blocks of block_keys, and each workgroup has an
+// equal stretch of that line, whatever lengths it falls on: it ends with the others, and the work of a compute unit is bounded by nothing but what its
+// memory can bring.  A sequence's head that lies in several stretches is as many parts; who has its last block notes how many.
+struct NoLds {};
+template <int D, int RB, bool E4M3, bool FRONT>
+__global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttnArgs a) {
+    __shared__ union {
+        RowsLds<D, RB> rows;
+        std::conditional_t<FRONT, TilesLds<D, 4>, NoLds> tiles;
+    } sh;
+    const int KH = a.cache.kv_heads;
+    if constexpr (FRONT) if ((int)blockIdx.x < a.front_blocks) {
+        constexpr int kHalves = D / TilesLds<D, 4>::DV;
+        const int kh = blockIdx.x % KH, rest = blockIdx.x / KH / kHalves, half = blockIdx.x / KH % kHalves;
+        const int groups = (a.seqs.n_tokens * a.group + 127) / 128;
+        attend_tiles<D, 4, E4M3>(a, front_span(a, rest / groups), kh, half, rest % groups * 128, sh.tiles);
+        return;
+    }
+    const int me = blockIdx.x - a.front_blocks;
+    if (!a.block_keys) {                                          // a workgroup for each
+        const Span p = own_span(a, me / KH, seq_at(a.seqs, me / KH), 0);
+        if (p.rows > 0) attend_rows<D, RB, E4M3>(a, p, me % KH, sh.rows);
+        return;
+    }
+    const int lane = threadIdx.x & 63, base = a.prefix & ~31;
+    const auto blocks_in = [&](const Seq& q) { return q.n > 0 && q.len > a.prefix ? (q.len - base + a.block_keys - 1) / a.block_keys : 0; };
+    // blocks of 64 sequences from s0 on, one a lane, and their sums up to each
+    const auto sums_of = [&](int s0, int* upto) {
+        const int n = s0 + lane < a.seqs.n_seqs ? blocks_in(seq_at(a.seqs, s0 + lane)) : 0;
+        int sum = n;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const int other = __shfl_up(sum, m);
+            if (lane >= m) sum += other;
+        }
+        *upto = sum;
+        return n;
+    };
+    int s = 0, unit = 0, total, n0 = 0, upto0 = 0;                // the sequence of the next block, and where its head's blocks begin
+    Seq q = seq_at(a.seqs, 0);
+    if (a.seqs.n_seqs == 1) {
+        total = blocks_in(q) * KH;
+    } else {
+        n0 = sums_of(0, &upto0);
+        total = __builtin_amdgcn_readlane(upto0, 63);
+        for (int s0 = 64; s0 < a.seqs.n_seqs; s0 += 64) {
+            int upto;
+            sums_of(s0, &upto);
+            total += __builtin_amdgcn_readlane(upto, 63);
+        }
+        total *= KH;
+    }
+    const int stretch = max((total + a.own_blocks - 1) / a.own_blocks, a.least_blocks);
+    if (total == 0 || me > (total - 1) / stretch) return;
+    const int stop = min(me * stretch + stretch, total);
+    int at = me * stretch;                                        // the next block
+    if (a.seqs.n_seqs > 1) {
+        for (int s0 = 0, before = 0; s0 < a.seqs.n_seqs; s0 += 64) {
+            const uint64_t there = __ballot(before + KH * upto0 > at);
+            if (there) {
+                const int which = __builtin_ctzll(there);
+                s = s0 + which;
+                unit = before + KH * (__builtin_amdgcn_readlane(upto0, which) - __builtin_amdgcn_readlane(n0, which));
+                break;
+            }
+            before += KH * __builtin_amdgcn_readlane(upto0, 63);
+            n0 = sums_of(s0 + 64, &upto0);
+        }
+        q = seq_at(a.seqs, s);
+    }
+    int n = blocks_in(q);
+    if (n == 0) return;                                           // (there is one: total is not 0)
+    int kh = (at - unit) / n;
+    unit += kh * n;
+    while (true) {
+        const int from = at - unit, take = min(n - from, stop - at), part = me - unit / stretch;
+        Span p = own_span(a, s, q, 0);
+        p.begin = base + from * a.block_keys;
+        p.end = min(p.end, p.begin + take * a.block_keys);
+        p.part = a.prefix_parts == 0 && take == n ? -1 : a.prefix_parts + part;
+        if (from + take == n && threadIdx.x == 0) as_global_out(a.unit_parts)[s * KH + kh] = part + 1;
+        attend_rows<D, RB, E4M3>(a, p, kh, sh.rows);
+        at += take;
+        if (at >= stop) return;
+        __syncthreads();
+        unit += n;
+        if (++kh == KH) {
+            kh = 0;
+            do {
+                if (++s >= a.seqs.n_seqs) return;                 // (there is one more, as at < total)
+                q = seq_at(a.seqs, s);
+                n = blocks_in(q);
+            } while (n == 0);
+        }
+    }
+}
+
 // The parts of a row: D / 4 threads hold a part's row, so that a workgroup's other threads take other parts; every load is there before one is needed.  Each
 // group of threads adds its parts in their order, then the groups' sums are added in theirs.
 template <int D>
@@ -717,13 +826,12 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const AttnArgs a) {
     __shared__ f32x4_t sh_acc[kGroups][kLanes];
     const int64_t rows = (int64_t)a.seqs.n_tokens * a.heads, row = (int64_t)blockIdx.x * a.heads + blockIdx.y;
     const int t = blockIdx.x, head = blockIdx.y;
-    const Seq q = seq_at(a.seqs, seq_of(a.seqs, t));
+    const int seq = seq_of(a.seqs, t);
+    const Seq q = seq_at(a.seqs, seq);
     if (t - q.first >= q.n) return;                           // no sequence has this token
-    const int own = own_parts(a, q.len);
-    if (a.prefix_parts == 0 && own <= 1) return;              // written by the workgroup itself
-    // own parts behind the row's position are left out: nothing in them is seen
-    const int pos = q.pos0 + t - q.first, base = a.prefix & ~31;
-    const int parts = a.prefix_parts + (pos < base ? 0 : min(own, (pos - base) / a.own_chunk + 1));
+    const int own = !a.block_keys ? own_parts(a, q.len) : q.len <= a.prefix ? 0 : as_global(a.unit_parts)[seq * a.cache.kv_heads + head / a.group];
+    if (a.prefix_parts == 0 && (own == 1 || (own == 0 && !a.block_keys))) return;     // written by the workgroup itself
+    const int parts = a.prefix_parts + own;
     float top = kNone;
     for (int i = threadIdx.x; i < parts; i += 256) top = fmaxf(top, as_global(a.part_ml)[2 * (i * rows + row)]);
 #pragma unroll
@@ -760,69 +868,96 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const AttnArgs a) {
 static int rows_of_block(int64_t rows, int head_dim) {
     if (rows <= 16) return 16;
     if (rows <= 32 && head_dim <= 128) return 32;
-    
     return rows <= 128 ? 128 : 256;
-
-}
-
-// Keys that a workgroup takes, so that a launch over `keys` of them for `units` sequences, key heads and blocks of rows is two workgroups of four wavefronts
-// on each compute unit (or one of eight), all of them there at once.  One sequence of 65000 keys, 8 key heads of 128: 512 workgroups 56.5 us, 1024 62.2;
-// 64 rows behind 8192 shared keys 109 and 154; 29 ragged sequences of up to 8000 64.6 and 65.3.  Where that is a whole batch at decoding the longest is cut up
-// all the same, as the others may be shorter.
-static int64_t chunk_of(int64_t keys, int64_t units, int block, int64_t grid_units) {
-    constexpr int64_t kMostGroups = (int64_t)1 << 22;         // workgroups in x: far from the 2^32 threads that one may have there
-    const int64_t wanted = block == 256 ? 256 : 512, least = 256, most = block <= 32 ? 4096 : keys;
-    int64_t chunk = (keys * units + wanted - 1) / wanted;
-    chunk = std::min(std::max(chunk, least), std::max(most, least));
-    if (keys / chunk > kMostGroups / grid_units) chunk = keys / std::max<int64_t>(kMostGroups / grid_units, 1) + 1;
-    return (chunk + 127) / 128 * 128;
 }
 
 static inline int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+static inline int64_t over(int64_t x, int64_t m) { return (x + m - 1) / m; }
+
+constexpr int64_t kResident = 512;                            // workgroups of four wavefronts, two on each compute unit, that are there at once
+constexpr int64_t kMostGroups = (int64_t)1 << 22;             // workgroups in x: far from the 2^32 threads that one launch may have there
+
+// Keys that a workgroup takes, so that a launch over `keys` of them for `units` sequences, key heads and blocks of 128 rows or more fills the chip once.
+static int64_t chunk_of(int64_t keys, int64_t units, int block, int64_t grid_units) {
+    int64_t chunk = std::max(std::min(over(keys * units, block == 256 ? kResident / 2 : kResident), keys), (int64_t)256);
+    if (keys / chunk > kMostGroups / grid_units) chunk = keys / std::max<int64_t>(kMostGroups / grid_units, 1) + 1;
+    return up_to(chunk, 128);
+}
 
 size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     const int D = a->cache.head_dim, heads = a->cache.kv_heads;
-    const int64_t rows = (int64_t)a->seqs.n_tokens * a->heads;
-    const size_t per_part = (size_t)rows * (D + 2) * 4;
-    const int64_t most = ws_bytes < 16 ? 0 : (int64_t)((ws_bytes - 16) / per_part);      // parts that the workspace holds
-    a->prefix_parts = 0;
-    a->parts = 1;
-    if (a->prefix > a->seqs.max_kv) a->prefix = a->seqs.max_kv;
-    const auto blocks = [&](int64_t tokens, int block) { return (tokens * a->group + block - 1) / block; };
-    const int block = rows_of_block((int64_t)a->seqs.max_q * a->group, D);
+    const int64_t rows = (int64_t)a->seqs.n_tokens * a->heads, notes = (int64_t)a->seqs.n_seqs * heads;
+    const int64_t per_part = rows * (D + 2) * 4, room = (int64_t)std::min<size_t>(ws_bytes, (size_t)1 << 60) - 4 * up_to(notes, 4) - 16;
+    const int64_t most = room > 0 ? room / per_part : 0;      // parts that the workspace holds
+    const auto blocks = [&](int64_t tokens, int block) { return over(tokens * a->group, block); };
     const auto halves = [&](int block) { return D == 256 && block >= 128 ? 2 : 1; };      // workgroups of such a block
+    const int block = rows_of_block((int64_t)a->seqs.max_q * a->group, D);
     const int64_t units = blocks(a->seqs.max_q, block) * heads * halves(block);
+    a->few = block <= 32;
+    a->prefix_parts = a->front_blocks = a->block_keys = 0;
+    if (a->prefix > a->seqs.max_kv) a->prefix = a->seqs.max_kv;
     // Every sequence reads the shared keys as its own where it has to, and where blocks of 128 rows and more, for which reading keys is little of the work, fill
     // the chip without being cut: 32 pieces of 64 tokens, 8 key heads of 4 query heads, behind 2048 shared keys 100 us so, 211 in parts; 6 pieces of 200
     // tokens (192 workgroups) 130 and 109, 8 of 70 behind 8192 (128) 176 and 133.
-    if (most < 2 || a->seqs.n_seqs < 2 || (block >= 128 && units * a->seqs.n_seqs >= 256)) a->prefix = 0;
-    int64_t prefix_parts = 0;
-    if (a->prefix) {
-        const int front = rows_of_block((int64_t)a->seqs.n_tokens * a->group, D);
-        const int64_t front_units = blocks(a->seqs.n_tokens, front) * heads * halves(front);
-        int64_t chunk = chunk_of(a->prefix, front_units, front, front_units);
-        if ((a->prefix + chunk - 1) / chunk > most / 2) chunk = up_to((a->prefix + most / 2 - 1) / (most / 2), 128);
-        a->prefix_chunk = (int)chunk;
-        prefix_parts = (a->prefix + chunk - 1) / chunk;
+    if (most < 3 || a->seqs.n_seqs < 2 || (!a->few && units * a->seqs.n_seqs >= 256)) a->prefix = 0;
+    const int64_t own = a->seqs.max_kv - (a->prefix & ~31);
+    const int front = a->few ? 128 : rows_of_block((int64_t)a->seqs.n_tokens * a->group, D);
+    const int64_t front_units = blocks(a->seqs.n_tokens, front) * heads * halves(front);
+    int64_t own_parts = 1;
+    if (a->few) {
+        int64_t cut = 128;                                    // keys in a block of the line; its blocks are counted in 32 bits
+        while ((over(own, cut) + 1) * notes >= (int64_t)1 << 29) cut *= 2;
+        int64_t own_blocks = kResident;
+        if (a->prefix) {
+            // What both cost in workgroups' time where all share the memory, in us: 64 keys for 128 rows of the front 3, 128 keys of a sequence 7 (heads of 128 in
+            // bf16); the longest sequence is known, and the others are taken to be half as long on the whole.
+            const double f = 3.0 * front_units * over(a->prefix, 64), o = (a->cache.e4m3 ? 3.5 : 7.0) * 0.5 * notes * over(std::max<int64_t>(own, 1), 128);
+            const int64_t share = (int64_t)(kResident * f / (f + o));
+            int64_t parts = std::max<int64_t>(over(share, front_units), 1);
+            parts = std::min(std::min(parts, over(a->prefix, 128)), std::min(most - 2, std::max<int64_t>(kMostGroups / front_units, 1)));
+            a->prefix_chunk = (int)up_to(over(a->prefix, parts), 128);
+            a->prefix_parts = (int)over(a->prefix, a->prefix_chunk);
+            a->front_blocks = (int)(a->prefix_parts * front_units);
+            own_blocks = std::max<int64_t>(kResident - a->front_blocks, kResident / 4);
+        }
+        const int64_t longest = over(own, cut), wanted = std::max<int64_t>(own_blocks / heads + 2, 4);
+        // as many parts as one sequence of nearly all keys would be, if that is not beyond the workspace or 128 MB
+        own_parts = std::min(std::min(most - a->prefix_parts, wanted), std::max<int64_t>(((int64_t)128 << 20) / per_part, 4));
+        if (own_parts >= 2) {
+            a->block_keys = (int)cut;
+            a->own_blocks = (int)own_blocks;
+            a->least_blocks = (int)std::max<int64_t>(over(longest, own_parts - 1), 1);      // a head in a stretch and part of another two, then, at most own_parts
+        } else {
+            own_parts = 1;
+        }
+        a->own_chunk = (int)up_to(std::max<int64_t>(own, 1), 128);
+    } else {
+        if (a->prefix) {
+            int64_t chunk = chunk_of(a->prefix, front_units, front, front_units);
+            if (over(a->prefix, chunk) > most / 2) chunk = up_to(over(a->prefix, most / 2), 128);
+            a->prefix_chunk = (int)chunk;
+            a->prefix_parts = (int)over(a->prefix, chunk);
+        }
+        const int64_t left = most - a->prefix_parts;
+        int64_t chunk = chunk_of(own, units * a->seqs.n_seqs, block, units);
+        if (left < 2 && !a->prefix) chunk = up_to(std::max<int64_t>(own, 1), 128);
+        else if (over(own, chunk) > left) chunk = up_to(over(own, left), 128);
+        a->own_chunk = (int)chunk;
+        own_parts = std::max<int64_t>(over(own, chunk), 1);
     }
-    const int64_t own = a->seqs.max_kv - (a->prefix & ~31), left = most - prefix_parts;
-    int64_t chunk = chunk_of(own, units * a->seqs.n_seqs, block, units);
-    if (left < 2 && !a->prefix) chunk = up_to(own > 0 ? own : 1, 128);
-    else if ((own + chunk - 1) / chunk > left) chunk = up_to((own + left - 1) / left, 128);
-    a->own_chunk = (int)chunk;
-    const int64_t own_most = own > 0 ? (own + chunk - 1) / chunk : 1;
-    a->prefix_parts = (int)prefix_parts;
-    a->parts = (int)(prefix_parts + own_most);
+    a->parts = (int)(a->prefix_parts + own_parts);
     if (a->parts == 1) return 0;
-    a->part_o = a->part_ml + 2 * up_to(a->parts * rows, 2);
-    return (size_t)(2 * up_to(a->parts * rows, 2) + (int64_t)a->parts * rows * D) * 4;
+    float* at = a->part_ml + 2 * up_to(a->parts * rows, 2);
+    a->part_o = at;
+    a->unit_parts = reinterpret_cast<int*>(at + (int64_t)a->parts * rows * D);
+    return (size_t)(2 * up_to(a->parts * rows, 2) + (int64_t)a->parts * rows * D + up_to(notes, 4)) * 4;
 }
 
 template <int D, int RB, bool E4M3>
-static void launch_rows(const AttnArgs& a, int front, hipStream_t stream) {
-    const int tokens = front ? a.seqs.n_tokens : a.seqs.max_q, parts = front ? a.prefix_parts : a.parts - a.prefix_parts;
-    const unsigned groups = (unsigned)(((int64_t)tokens * a.group + 16 * RB - 1) / (16 * RB));
-    attend_rows_kernel<D, RB, E4M3><<<dim3(parts * groups, (unsigned)a.cache.kv_heads, front ? 1u : (unsigned)a.seqs.n_seqs), 256, 0, stream>>>(a, front);
+static void launch_few(const AttnArgs& a, hipStream_t stream) {
+    const int64_t own = a.block_keys ? a.own_blocks : (int64_t)a.seqs.n_seqs * a.cache.kv_heads;
+    if (a.front_blocks) attend_few_kernel<D, RB, E4M3, true><<<(unsigned)(a.front_blocks + own), 256, 0, stream>>>(a);
+    else attend_few_kernel<D, RB, E4M3, false><<<(unsigned)own, 256, 0, stream>>>(a);
 }
 
 template <int D, int NW, bool E4M3>
@@ -834,11 +969,14 @@ static void launch_tiles(const AttnArgs& a, int front, hipStream_t stream) {
 
 template <int D, bool E4M3>
 static void launch_rows_of(const AttnArgs& a, hipStream_t stream) {
+    if (a.few) {
+        if (a.seqs.max_q * (int64_t)a.group <= 16) launch_few<D, 1, E4M3>(a, stream);
+        else launch_few<D, D == 256 ? 1 : 2, E4M3>(a, stream);
+        return;
+    }
     for (int front = a.prefix_parts ? 1 : 0; front >= 0; --front) {
         const int block = rows_of_block((int64_t)(front ? a.seqs.n_tokens : a.seqs.max_q) * a.group, D);
-        if (block == 16) launch_rows<D, 1, E4M3>(a, front, stream);
-        else if (block == 32) launch_rows<D, D == 256 ? 1 : 2, E4M3>(a, front, stream);
-        else if (block == 128) launch_tiles<D, 4, E4M3>(a, front, stream);
+        if (block <= 128) launch_tiles<D, 4, E4M3>(a, front, stream);
         else launch_tiles<D, 8, E4M3>(a, front, stream);
     }
 }
