@@ -58,9 +58,9 @@ struct AttnArgs {
     int own_chunk;            // keys of a sequence's own that one workgroup takes: a multiple of 128, counted from prefix rounded down to 32
     int prefix_chunk, prefix_parts;
     int parts;                // prefix_parts + the most that a sequence's own keys are; 1: workgroups write O, else partial results
-    // few rows a sequence: one launch of front_blocks workgroups for the shared front and own_blocks that have equal stretches (least_blocks at least) of all
-    // own keys, in blocks of block_keys; 0: a workgroup for each sequence and key head
-    int few, front_blocks, own_blocks, block_keys, least_blocks;
+    // few rows a sequence: one launch of front_blocks workgroups for the shared front and line_waves wavefronts that have equal stretches (least_steps at least)
+    // of all own keys, in steps of 32; 0: a workgroup for each sequence and key head
+    int few, front_blocks, line_waves, least_steps;
     float* part_ml;           // parts x n_tokens x heads pairs: running maximum (of scores times log2(e)) and sum
     float* part_o;            // parts x n_tokens x heads x head_dim
     int* unit_parts;          // n_seqs x kv_heads: the parts of its own keys

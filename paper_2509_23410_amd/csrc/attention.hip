@@ -10,7 +10,6 @@
 // both, and the second product's B operand is what the lane already holds of the first's result, if the keys of a step are given out to the rows of A
 // in the right order: no value of P crosses lanes.  V lies feature-major in its pages, so V^T's operand is a plain 16-byte load too.
 #include <algorithm>
-#include <type_traits>
 
 #include "cells.h"
 
@@ -77,7 +76,7 @@ __device__ __forceinline__ Span own_span(const AttnArgs& a, int s, const Seq& q,
     p.key0 = a.prefix;
     p.key1 = max(q.len, a.prefix);
     p.begin = (a.prefix & ~31) + chunk * a.own_chunk;
-    p.end = a.block_keys ? q.len : min(q.len, p.begin + a.own_chunk);
+    p.end = a.line_waves ? q.len : min(q.len, p.begin + a.own_chunk);
     p.part = a.parts == 1 || (a.prefix_parts == 0 && q.len - p.begin <= a.own_chunk && chunk == 0) ? -1 : a.prefix_parts + chunk;
     p.table = s * a.seqs.table_stride;
     p.bad = q.bad;
@@ -199,16 +198,17 @@ struct KeyRegs {
     u32x4_t v[E4M3 ? D / 32 : D / 16];
 };
 
+// Row i of A's tile b is key 8 (i / 4) + 4 b + i % 4 of a step: a lane then holds, of both tiles, the keys 8 g .. 8 g + 7 of its column.
+__device__ __forceinline__ int key_of_row(int row) { return 8 * (row >> 2) + (row & 3); }
+
+// A step's cells: k_page is the page of the lane's key in K, v_page that of its eight keys in V (both in range)
 template <int D, bool E4M3>
-__device__ __forceinline__ void load_keys(KeyRegs<D, E4M3>& r, const AttnArgs& a, const int* pages, int step, int kh, int lane) {
+__device__ __forceinline__ void load_cells(KeyRegs<D, E4M3>& r, const AttnArgs& a, int k_page, int v_page, int step, int kh, int lane) {
     constexpr int kCell = E4M3 ? 1 : 2;
     const int g = lane >> 4, row = lane & 15, mask = (1 << a.cache.page_log2) - 1;
-    // row i of A's tile b is key 8 (i / 4) + 4 b + i % 4: a lane then holds, of both tiles, the keys 8 g .. 8 g + 7 of its column
-    const int key = 8 * (row >> 2) + (row & 3);
     {
-        const int at = step + key;
-        const int page = max(pages[at >> a.cache.page_log2], 0);
-        const PATCH_EP_GLOBAL uint8_t* base = as_global(a.cache.k) + page * a.cache.page_bytes + (((int64_t)kh << a.cache.page_log2) + (at & mask)) * (D * kCell) + 16 * g;
+        const int at = step + key_of_row(row);
+        const PATCH_EP_GLOBAL uint8_t* base = as_global(a.cache.k) + k_page * a.cache.page_bytes + (((int64_t)kh << a.cache.page_log2) + (at & mask)) * (D * kCell) + 16 * g;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -217,8 +217,7 @@ __device__ __forceinline__ void load_keys(KeyRegs<D, E4M3>& r, const AttnArgs& a
     }
     {
         const int at = step + 8 * g;
-        const int page = max(pages[at >> a.cache.page_log2], 0);
-        const PATCH_EP_GLOBAL uint8_t* base = as_global(a.cache.v) + page * a.cache.page_bytes + ((((int64_t)kh * D + row) << a.cache.page_log2) + (at & mask)) * kCell;
+        const PATCH_EP_GLOBAL uint8_t* base = as_global(a.cache.v) + v_page * a.cache.page_bytes + ((((int64_t)kh * D + row) << a.cache.page_log2) + (at & mask)) * kCell;
         const int64_t next = (int64_t)(16 * kCell) << a.cache.page_log2;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
@@ -232,6 +231,10 @@ __device__ __forceinline__ void load_keys(KeyRegs<D, E4M3>& r, const AttnArgs& a
         }
     }
 }
+template <int D, bool E4M3>
+__device__ __forceinline__ void load_keys(KeyRegs<D, E4M3>& r, const AttnArgs& a, const int* pages, int step, int kh, int lane) {
+    load_cells<D, E4M3>(r, a, max(pages[(step + key_of_row(lane & 15)) >> a.cache.page_log2], 0), max(pages[(step + 8 * (lane >> 4)) >> a.cache.page_log2], 0), step, kh, lane);
+}
 
 // the operand of 32 of a head's values (i counts them) for keys of tile b; in e4m3 a 16-byte load is the operands of two products, and Q's follow it
 template <int D, bool E4M3>
@@ -242,34 +245,96 @@ __device__ __forceinline__ bf16x8_t key_operand(const KeyRegs<D, E4M3>& r, int b
 template <bool E4M3>
 __device__ __forceinline__ int query_offset(int i, int g) { return E4M3 ? 64 * (i / 2) + 16 * g + 8 * (i % 2) : 32 * i + 8 * g; }
 
-template <int D, int RB>
-struct RowsLds {
-    float o[4][16][D + 4], m[4][RB * 16], l[4][RB * 16];
-    int pages[kTableKeys / 16];
+// What a wavefront has of its rows: running maxima (the same in all lanes of a column), sums (each lane its own keys'), and O^T.
+template <int D, int RB, bool E4M3>
+struct RowState {
+    f32x4_t o[RB][D / 16];
+    float m[RB], l[RB];
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            m[b] = kNone;
+            l[b] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) o[b][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+
+    // A step of 32 keys; `none`: the lane's eight keys have no page.  Returns whether values that are not finite and that not every row sees went into O.
+    __device__ __forceinline__ bool step(const bf16x8_t (&q)[RB][D / 32], const KeyRegs<D, E4M3>& kv, const Span& p, int step, bool none, const int (&limit)[RB], int fewest,
+                                         float scale, int lane) {
+        const int g = lane >> 4;
+        f32x4_t s[RB][2];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) s[b][0] = s[b][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bf16x8_t k = key_operand<D, E4M3>(kv, h, i);
+#pragma unroll
+                for (int b = 0; b < RB; ++b) s[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[b][i], s[b][h], 0, 0, 0);
+            }
+        const bool ragged = step < p.key0 || step + 32 > fewest || step + 32 > p.key1 || __any(none);
+        const int key = step + 8 * g;                       // the lane's eight keys
+        bf16x8_t pr[RB];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = s[b][e / 4][e % 4] * scale;
+            if (ragged) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[e] = key + e >= p.key0 && key + e < limit[b] ? (none ? __builtin_nanf("") : x[e]) : kNone;
+            }
+            float top = x[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+            if (__any(top > m[b] + kRise)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float m_new = fmaxf(m[b], top), down = exp2_off(m[b], m_new);
+                m[b] = m_new;
+                l[b] *= down;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) o[b][i] = o[b][i] * down;
+            }
+            float sum = 0.f, y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                y[e] = exp2_off(x[e], m[b]);
+                sum += y[e];
+            }
+            l[b] += sum;
+            pr[b] = as_bf16x8(u32x4_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])});
+        }
+        u32x4_t v[D / 16];
+        bool infinite = false;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            if constexpr (E4M3) v[i] = widen8(kv.v[i / 2][2 * (i % 2)], kv.v[i / 2][2 * (i % 2) + 1]);
+            else v[i] = kv.v[i];
+            if (ragged) {                                    // cells that no key is in may hold anything, and 0 times a NaN is one
+                keep_keys(v[i], key, p.key0, p.key1);
+                infinite |= any_infinite(v[i]);
+            }
+        }
+        // ... and so may keys that only some of the rows see
+        const bool redo = ragged && fewest < min(step + 32, p.key1) && infinite;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v[i]), pr[b], o[b][i], 0, 0, 0);
+        return redo;
+    }
 };
 
-// All rows of a span (16 RB at most), by a workgroup of four wavefronts.
+// The queries of rows 0 .. 16 RB - 1 of a span, as the first product's operand.
 template <int D, int RB, bool E4M3>
-__device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, int kh, RowsLds<D, RB>& sh) {
-    constexpr bool kAhead = D * RB <= 128;      // with more, two steps' keys do not fit beside the rest in half a SIMD's registers
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
-    int limit[RB], fewest = 0x7FFFFFFF, most = 0;
-#pragma unroll
-    for (int b = 0; b < RB; ++b) {
-        const int r = 16 * b + col;
-        limit[b] = row_limit(a, p, r);
-        if (r < p.rows) fewest = min(fewest, limit[b]);
-        most = max(most, limit[b]);
-    }
-#pragma unroll
-    for (int m = 1; m < 16; m <<= 1) {
-        fewest = min(fewest, __shfl_xor(fewest, m));
-        most = max(most, __shfl_xor(most, m));
-    }
-    fewest = __builtin_amdgcn_readfirstlane(fewest);
-    const int end = __builtin_amdgcn_readfirstlane(min(p.end, most));
-
-    bf16x8_t q[RB][D / 32];
+__device__ __forceinline__ void load_queries(bf16x8_t (&q)[RB][D / 32], const AttnArgs& a, const Span& p, int kh, int lane) {
+    const int g = lane >> 4, col = lane & 15;
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
         const int r = 16 * b + col;
@@ -282,19 +347,48 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, in
             q[b][i] = as_bf16x8(v);
         }
     }
-    float scale = a.scale;
-    if (E4M3 && a.cache.k_scale) scale *= as_global(a.cache.k_scale)[kh];
+}
 
-    f32x4_t o[RB][D / 16];
-    float m[RB], l[RB];
+// The keys that the rows see: of each lane's columns, the fewest of any row, the most.
+template <int RB>
+__device__ __forceinline__ void row_limits(const AttnArgs& a, const Span& p, int lane, int (&limit)[RB], int* fewest, int* most) {
+    int few = 0x7FFFFFFF, many = 0;
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        m[b] = kNone;
-        l[b] = 0.f;
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) o[b][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        const int r = 16 * b + (lane & 15);
+        limit[b] = row_limit(a, p, r);
+        if (r < p.rows) few = min(few, limit[b]);
+        many = max(many, limit[b]);
     }
+#pragma unroll
+    for (int m = 1; m < 16; m <<= 1) {
+        few = min(few, __shfl_xor(few, m));
+        many = max(many, __shfl_xor(many, m));
+    }
+    *fewest = __builtin_amdgcn_readfirstlane(few);
+    *most = __builtin_amdgcn_readfirstlane(many);
+}
 
+template <int D, int RB>
+struct RowsLds {
+    float o[4][16][D + 4], m[4][RB * 16], l[4][RB * 16];
+    int pages[kTableKeys / 16];
+};
+
+// All rows of a span (16 RB at most), by a workgroup of four wavefronts.
+template <int D, int RB, bool E4M3>
+__device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, int kh, RowsLds<D, RB>& sh) {
+    constexpr bool kAhead = D * RB <= 128;      // with more, two steps' keys do not fit beside the rest in half a SIMD's registers
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
+    int limit[RB], fewest, most;
+    row_limits<RB>(a, p, lane, limit, &fewest, &most);
+    const int end = min(p.end, most);
+    bf16x8_t q[RB][D / 32];
+    load_queries<D, RB, E4M3>(q, a, p, kh, lane);
+    float scale = a.scale;
+    if (E4M3 && a.cache.k_scale) scale *= as_global(a.cache.k_scale)[kh];
+    RowState<D, RB, E4M3> st;
+    st.clear();
     bool redo = false;
     for (int window = p.begin; window < end; window += kTableKeys) {
         const int stop = min(end, window + kTableKeys);
@@ -311,70 +405,8 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, in
             KeyRegs<D, E4M3> kv = next;
             if constexpr (kAhead) load_keys<D, E4M3>(next, a, pages, min(step + 128, last_step), kh, lane);
             else load_keys<D, E4M3>(kv, a, pages, step, kh, lane);
-            f32x4_t s[RB][2];
-#pragma unroll
-            for (int b = 0; b < RB; ++b) s[b][0] = s[b][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const bf16x8_t k = key_operand<D, E4M3>(kv, h, i);
-#pragma unroll
-                    for (int b = 0; b < RB; ++b) s[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[b][i], s[b][h], 0, 0, 0);
-                }
-            const bool ragged = step < p.key0 || step + 32 > fewest || step + 32 > p.key1 || p.bad ||
-                                (pages[step >> a.cache.page_log2] | pages[(step + 16) >> a.cache.page_log2]) < 0;
-            const int key = step + 8 * g;                       // the lane's eight keys
-            bf16x8_t pr[RB];
-#pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = s[b][e / 4][e % 4] * scale;
-                if (ragged) {
-                    const bool bad = p.bad || pages[key >> a.cache.page_log2] < 0;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        x[e] = key + e >= p.key0 && key + e < limit[b] ? (bad ? __builtin_nanf("") : x[e]) : kNone;
-                }
-                float top = x[0];
-#pragma unroll
-                for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
-                if (__any(top > m[b] + kRise)) {
-                    top = fmaxf(top, __shfl_xor(top, 16));
-                    top = fmaxf(top, __shfl_xor(top, 32));
-                    const float m_new = fmaxf(m[b], top), down = exp2_off(m[b], m_new);
-                    m[b] = m_new;
-                    l[b] *= down;
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i) o[b][i] = o[b][i] * down;
-                }
-                float sum = 0.f, y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    y[e] = exp2_off(x[e], m[b]);
-                    sum += y[e];
-                }
-                l[b] += sum;
-                pr[b] = as_bf16x8(u32x4_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])});
-            }
-            u32x4_t v[D / 16];
-            bool infinite = false;
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-                if constexpr (E4M3) v[i] = widen8(kv.v[i / 2][2 * (i % 2)], kv.v[i / 2][2 * (i % 2) + 1]);
-                else v[i] = kv.v[i];
-                if (ragged) {                                    // cells that no key is in may hold anything, and 0 times a NaN is one
-                    keep_keys(v[i], key, p.key0, p.key1);
-                    infinite |= any_infinite(v[i]);
-                }
-            }
-            // ... and so may keys that only some of the rows see
-            redo |= ragged && fewest < min(step + 32, p.key1) && infinite;
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v[i]), pr[b], o[b][i], 0, 0, 0);
+            const bool none = p.bad || pages[(step + 8 * g) >> a.cache.page_log2] < 0;
+            redo |= st.step(q, kv, p, step, none, limit, fewest, scale, lane);
         }
     }
     if (__syncthreads_or(redo)) {
@@ -385,11 +417,11 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, in
     // the four wavefronts' results: rows of a block of 16 at a time, 16 threads a row
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        l[b] += __shfl_xor(l[b], 16);
-        l[b] += __shfl_xor(l[b], 32);
+        st.l[b] += __shfl_xor(st.l[b], 16);
+        st.l[b] += __shfl_xor(st.l[b], 32);
         if (g == 0) {
-            sh.m[wave][16 * b + col] = m[b];
-            sh.l[wave][16 * b + col] = l[b];
+            sh.m[wave][16 * b + col] = st.m[b];
+            sh.l[wave][16 * b + col] = st.l[b];
         }
     }
     float v_scale = 1.f;
@@ -400,9 +432,9 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, in
         float top = kNone;
 #pragma unroll
         for (int w = 0; w < 4; ++w) top = fmaxf(top, sh.m[w][16 * b + col]);
-        const float down = exp2_off(m[b], top);
+        const float down = exp2_off(st.m[b], top);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4_t*>(&sh.o[wave][col][16 * i + 4 * g]) = o[b][i] * down;
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4_t*>(&sh.o[wave][col][16 * i + 4 * g]) = st.o[b][i] * down;
         __syncthreads();
         const int c = threadIdx.x / 16, d0 = (threadIdx.x % 16) * (D / 16), r = 16 * b + c;
         if (r < p.rows) {
@@ -719,36 +751,31 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs
     attend_tiles<D, NW, E4M3>(a, p, kh, half, first_row, sh);
 }
 
-// Few rows a sequence: the first front_blocks workgroups have the shared front, for all rows (in blocks of 128); beside them, on the same compute units, the
-// others have the sequences' own keys.  Those are one line, sequence by sequence and head by head in it, in blocks of block_keys, and each workgroup has an
-// equal stretch of that line, whatever lengths it falls on: it ends with the others, and the work of a compute unit is bounded by nothing but what its
-// memory can bring.  A sequence's head that lies in several stretches is as many parts; who has its last block notes how many.
-struct NoLds {};
-template <int D, int RB, bool E4M3, bool FRONT>
-__global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttnArgs a) {
-    __shared__ union {
-        RowsLds<D, RB> rows;
-        std::conditional_t<FRONT, TilesLds<D, 4>, NoLds> tiles;
-    } sh;
-    const int KH = a.cache.kv_heads;
-    if constexpr (FRONT) if ((int)blockIdx.x < a.front_blocks) {
-        constexpr int kHalves = D / TilesLds<D, 4>::DV;
-        const int kh = blockIdx.x % KH, rest = blockIdx.x / KH / kHalves, half = blockIdx.x / KH % kHalves;
-        const int groups = (a.seqs.n_tokens * a.group + 127) / 128;
-        attend_tiles<D, 4, E4M3>(a, front_span(a, rest / groups), kh, half, rest % groups * 128, sh.tiles);
-        return;
-    }
-    const int me = blockIdx.x - a.front_blocks;
-    if (!a.block_keys) {                                          // a workgroup for each
-        const Span p = own_span(a, me / KH, seq_at(a.seqs, me / KH), 0);
-        if (p.rows > 0) attend_rows<D, RB, E4M3>(a, p, me % KH, sh.rows);
-        return;
-    }
-    const int lane = threadIdx.x & 63, base = a.prefix & ~31;
-    const auto blocks_in = [&](const Seq& q) { return q.n > 0 && q.len > a.prefix ? (q.len - base + a.block_keys - 1) / a.block_keys : 0; };
-    // blocks of 64 sequences from s0 on, one a lane, and their sums up to each
+// Few rows a sequence and nowhere to put parts: a workgroup for each sequence and key head.
+template <int D, int RB, bool E4M3>
+__global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttnArgs a) {
+    __shared__ RowsLds<D, RB> sh;
+    const int s = blockIdx.x / a.cache.kv_heads;
+    const Span p = own_span(a, s, seq_at(a.seqs, s), 0);
+    if (p.rows > 0) attend_rows<D, RB, E4M3>(a, p, blockIdx.x % a.cache.kv_heads, sh);
+}
+
+// A step of the line of all sequences' own keys: sequence by sequence, in it head by head, in that 32 keys at a time.
+struct Place {
+    Seq q;
+    int s, kh, n, i, unit;      // sequence, key head, steps of a head of it, which of them this is, and the line's number of the head's first
+};
+
+// The steps [me * stretch, + stretch) of the line, by one wavefront by itself: the keys of its next step, of whatever head, and the page numbers of the one
+// behind that are on their way while it works on one, and what it has of a head's rows it writes when that head or its stretch ends.
+template <int D, int RB, bool E4M3>
+__device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
+    constexpr bool kAhead = D * RB <= 128;
+    const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15, KH = a.cache.kv_heads, base = a.prefix & ~31;
+    const auto steps_in = [&](const Seq& q) { return q.n > 0 && q.len > a.prefix ? (q.len - base + 31) / 32 : 0; };
+    // steps of 64 sequences from s0 on, one a lane, and their sums up to each
     const auto sums_of = [&](int s0, int* upto) {
-        const int n = s0 + lane < a.seqs.n_seqs ? blocks_in(seq_at(a.seqs, s0 + lane)) : 0;
+        const int n = s0 + lane < a.seqs.n_seqs ? steps_in(seq_at(a.seqs, s0 + lane)) : 0;
         int sum = n;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
@@ -758,10 +785,12 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttnArgs a) {
         *upto = sum;
         return n;
     };
-    int s = 0, unit = 0, total, n0 = 0, upto0 = 0;                // the sequence of the next block, and where its head's blocks begin
-    Seq q = seq_at(a.seqs, 0);
+    Place c;
+    c.s = c.unit = 0;
+    c.q = seq_at(a.seqs, 0);
+    int total, n0 = 0, upto0 = 0;
     if (a.seqs.n_seqs == 1) {
-        total = blocks_in(q) * KH;
+        total = steps_in(c.q) * KH;
     } else {
         n0 = sums_of(0, &upto0);
         total = __builtin_amdgcn_readlane(upto0, 63);
@@ -772,49 +801,163 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttnArgs a) {
         }
         total *= KH;
     }
-    const int stretch = max((total + a.own_blocks - 1) / a.own_blocks, a.least_blocks);
+    const int stretch = max((total + a.line_waves - 1) / a.line_waves, a.least_steps);
     if (total == 0 || me > (total - 1) / stretch) return;
-    const int stop = min(me * stretch + stretch, total);
-    int at = me * stretch;                                        // the next block
+    const int at = me * stretch, count = min(stretch, total - at);
     if (a.seqs.n_seqs > 1) {
         for (int s0 = 0, before = 0; s0 < a.seqs.n_seqs; s0 += 64) {
             const uint64_t there = __ballot(before + KH * upto0 > at);
             if (there) {
                 const int which = __builtin_ctzll(there);
-                s = s0 + which;
-                unit = before + KH * (__builtin_amdgcn_readlane(upto0, which) - __builtin_amdgcn_readlane(n0, which));
+                c.s = s0 + which;
+                c.unit = before + KH * (__builtin_amdgcn_readlane(upto0, which) - __builtin_amdgcn_readlane(n0, which));
                 break;
             }
             before += KH * __builtin_amdgcn_readlane(upto0, 63);
             n0 = sums_of(s0 + 64, &upto0);
         }
-        q = seq_at(a.seqs, s);
+        c.q = seq_at(a.seqs, c.s);
     }
-    int n = blocks_in(q);
-    if (n == 0) return;                                           // (there is one: total is not 0)
-    int kh = (at - unit) / n;
-    unit += kh * n;
-    while (true) {
-        const int from = at - unit, take = min(n - from, stop - at), part = me - unit / stretch;
-        Span p = own_span(a, s, q, 0);
-        p.begin = base + from * a.block_keys;
-        p.end = min(p.end, p.begin + take * a.block_keys);
-        p.part = a.prefix_parts == 0 && take == n ? -1 : a.prefix_parts + part;
-        if (from + take == n && threadIdx.x == 0) as_global_out(a.unit_parts)[s * KH + kh] = part + 1;
-        attend_rows<D, RB, E4M3>(a, p, kh, sh.rows);
-        at += take;
-        if (at >= stop) return;
-        __syncthreads();
-        unit += n;
-        if (++kh == KH) {
-            kh = 0;
-            do {
-                if (++s >= a.seqs.n_seqs) return;                 // (there is one more, as at < total)
-                q = seq_at(a.seqs, s);
-                n = blocks_in(q);
-            } while (n == 0);
+    c.n = steps_in(c.q);
+    if (c.n == 0) return;                                         // (there is one: total is not 0)
+    c.kh = (at - c.unit) / c.n;
+    c.unit += c.kh * c.n;
+    c.i = at - c.unit;
+
+    // goes to the step behind p, which there is
+    const auto go_on = [&](Place& p) {
+        if (++p.i < p.n) return;
+        p.i = 0;
+        p.unit += p.n;
+        if (++p.kh < KH) return;
+        p.kh = 0;
+        do {
+            p.s = min(p.s + 1, a.seqs.n_seqs - 1);
+            p.q = seq_at(a.seqs, p.s);
+            p.n = steps_in(p.q);
+        } while (p.n == 0 && p.s < a.seqs.n_seqs - 1);
+    };
+    // pages of the lane's key in K and of its keys in V: -1 where there is none
+    const auto ask_pages = [&](const Place& p, int* k_page, int* v_page) {
+        const int k_key = base + 32 * p.i + key_of_row(col), v_key = base + 32 * p.i + 8 * g;
+        const PATCH_EP_GLOBAL int32_t* row = as_global(a.seqs.table) + p.s * a.seqs.table_stride;
+        *k_page = *v_page = -1;
+        if (k_key < p.q.len) *k_page = row[k_key >> a.cache.page_log2];
+        if (v_key < p.q.len) *v_page = row[v_key >> a.cache.page_log2];
+    };
+    const auto checked = [&](const Place& p, int id) { return p.q.bad ? -1 : page_or_none(id, a.cache.n_pages); };
+
+    int token_of[RB], head_of[RB];                                // of the lane's columns
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        token_of[b] = (16 * b + col) / a.group;
+        head_of[b] = (16 * b + col) % a.group;
+    }
+    bf16x8_t q[RB][D / 32];
+    int limit[RB];
+    float scale = 0.f;
+    RowState<D, RB, E4M3> st;
+    Span p;
+    bool redo = false;
+    // Loads come back in the order in which they were asked for: the page numbers of a step are asked for in front of the cells of the step before it, so that
+    // the wait for them is none for those.
+    KeyRegs<D, E4M3> next;
+    Place f = c;
+    if (count > 1) go_on(f);
+    int k_now, v_now, k_id, v_id;
+    ask_pages(c, &k_now, &v_now);
+    ask_pages(f, &k_id, &v_id);
+    k_now = checked(c, k_now);
+    v_now = checked(c, v_now);
+    if constexpr (kAhead) load_cells<D, E4M3>(next, a, max(k_now, 0), max(v_now, 0), base + 32 * c.i, c.kh, lane);
+    for (int t = 0; t < count; ++t) {
+        const int step = base + 32 * c.i;
+        if (t == 0 || c.i == 0) {                                 // a head's rows
+            p = own_span(a, c.s, c.q, 0);
+            p.begin = step;
+            scale = a.scale;
+            if (E4M3 && a.cache.k_scale) scale *= as_global(a.cache.k_scale)[c.kh];
+            load_queries<D, RB, E4M3>(q, a, p, c.kh, lane);
+#pragma unroll
+            for (int b = 0; b < RB; ++b) limit[b] = 16 * b + col < p.rows ? p.pos0 + token_of[b] + 1 : 0;
+            st.clear();
+            redo = false;
+        }
+        KeyRegs<D, E4M3> kv = next;
+        const bool none = v_now < 0;
+        if constexpr (!kAhead) load_cells<D, E4M3>(kv, a, max(k_now, 0), max(v_now, 0), step, c.kh, lane);
+        k_now = checked(f, k_id);
+        v_now = checked(f, v_id);
+        Place ff = f;
+        if (t + 2 < count) go_on(ff);
+        ask_pages(ff, &k_id, &v_id);
+        if constexpr (kAhead) load_cells<D, E4M3>(next, a, max(k_now, 0), max(v_now, 0), base + 32 * f.i, f.kh, lane);
+
+        redo |= st.step(q, kv, p, step, none, limit, p.pos0 + 1, scale, lane);
+
+        const bool ends = c.i == c.n - 1;
+        if (ends || t == count - 1) {
+            const int part = me - c.unit / stretch;
+            p.end = min(p.end, step + 32);
+            p.part = a.prefix_parts == 0 && ends && c.i <= t ? -1 : a.prefix_parts + part;      // all of the head's keys: the result itself
+            if (ends && lane == 0) as_global_out(a.unit_parts)[c.s * KH + c.kh] = part + 1;
+            if (__any(redo)) {
+                for (int r = 0; r < min(16 * RB, p.rows); ++r) attend_row_alone<D, E4M3>(a, p, c.kh, r, lane, nullptr, 0, D);
+            } else {
+                float v_scale = 1.f;
+                if (E4M3 && a.cache.v_scale) v_scale = as_global(a.cache.v_scale)[c.kh];
+#pragma unroll
+                for (int b = 0; b < RB; ++b) {
+                    float l = st.l[b];
+                    l += __shfl_xor(l, 16);
+                    l += __shfl_xor(l, 32);
+                    if (16 * b + col >= p.rows) continue;
+                    const int64_t token = p.t0 + token_of[b];
+                    const int head = c.kh * a.group + head_of[b];
+                    const int64_t row = token * a.heads + head, to = (int64_t)p.part * a.seqs.n_tokens * a.heads + row;
+                    const float over = (p.part < 0 ? (l == 0.f ? 0.f : 1.f / l) : 1.f) * v_scale;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const f32x4_t o = st.o[b][i] * over;
+                        if (p.part < 0)
+                            *reinterpret_cast<PATCH_EP_GLOBAL u32x2_t*>(as_global_out(a.O) + token * a.o_stride + (int64_t)head * D + 16 * i + 4 * g) =
+                                u32x2_t{bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};
+                        else
+                            *reinterpret_cast<PATCH_EP_GLOBAL f32x4_t*>(as_global_out(a.part_o) + to * D + 16 * i + 4 * g) = o;
+                    }
+                    if (g == 0) {
+                        if (p.part >= 0) {
+                            as_global_out(a.part_ml)[2 * to] = st.m[b];
+                            as_global_out(a.part_ml)[2 * to + 1] = l;
+                        } else if (a.lse) {
+                            as_global_out(a.lse)[row] = 0.6931471805599453f * (st.m[b] + __builtin_log2f(l));
+                        }
+                    }
+                }
+            }
+        }
+        c = f;
+        f = ff;
+    }
+}
+
+// Few rows a sequence: the first front_blocks workgroups have the shared front, for all rows (in blocks of 128); beside them, on the same compute units, the
+// others have the sequences' own keys.  Those are one line of steps, and each wavefront has an equal stretch of it, whatever lengths it falls on: it ends
+// with the others, and the work of a compute unit is bounded by nothing but what its memory can bring.  A sequence's head that lies in several stretches is
+// as many parts; who has its last step notes how many.
+template <int D, int RB, bool E4M3, bool FRONT>
+__global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttnArgs a) {
+    if constexpr (FRONT) {
+        __shared__ TilesLds<D, 4> sh;
+        constexpr int kHalves = D / TilesLds<D, 4>::DV;
+        if ((int)blockIdx.x < a.front_blocks) {
+            const int kh = blockIdx.x % a.cache.kv_heads, rest = blockIdx.x / a.cache.kv_heads / kHalves, half = blockIdx.x / a.cache.kv_heads % kHalves;
+            const int groups = (a.seqs.n_tokens * a.group + 127) / 128;
+            attend_tiles<D, 4, E4M3>(a, front_span(a, rest / groups), kh, half, rest % groups * 128, sh);
+            return;
         }
     }
+    attend_line<D, RB, E4M3>(a, __builtin_amdgcn_readfirstlane((blockIdx.x - a.front_blocks) * 4 + (threadIdx.x >> 6)));
 }
 
 // The parts of a row: D / 4 threads hold a part's row, so that a workgroup's other threads take other parts; every load is there before one is needed.  Each
@@ -829,8 +972,8 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const AttnArgs a) {
     const int seq = seq_of(a.seqs, t);
     const Seq q = seq_at(a.seqs, seq);
     if (t - q.first >= q.n) return;                           // no sequence has this token
-    const int own = !a.block_keys ? own_parts(a, q.len) : q.len <= a.prefix ? 0 : as_global(a.unit_parts)[seq * a.cache.kv_heads + head / a.group];
-    if (a.prefix_parts == 0 && (own == 1 || (own == 0 && !a.block_keys))) return;     // written by the workgroup itself
+    const int own = !a.line_waves ? own_parts(a, q.len) : q.len <= a.prefix ? 0 : as_global(a.unit_parts)[seq * a.cache.kv_heads + head / a.group];
+    if (a.prefix_parts == 0 && (own == 1 || (own == 0 && !a.line_waves))) return;     // written by the workgroup itself
     const int parts = a.prefix_parts + own;
     float top = kNone;
     for (int i = threadIdx.x; i < parts; i += 256) top = fmaxf(top, as_global(a.part_ml)[2 * (i * rows + row)]);
@@ -894,19 +1037,19 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     const int block = rows_of_block((int64_t)a->seqs.max_q * a->group, D);
     const int64_t units = blocks(a->seqs.max_q, block) * heads * halves(block);
     a->few = block <= 32;
-    a->prefix_parts = a->front_blocks = a->block_keys = 0;
+    a->prefix_parts = a->front_blocks = a->line_waves = 0;
     if (a->prefix > a->seqs.max_kv) a->prefix = a->seqs.max_kv;
     // Every sequence reads the shared keys as its own where it has to, and where blocks of 128 rows and more, for which reading keys is little of the work, fill
     // the chip without being cut: 32 pieces of 64 tokens, 8 key heads of 4 query heads, behind 2048 shared keys 100 us so, 211 in parts; 6 pieces of 200
     // tokens (192 workgroups) 130 and 109, 8 of 70 behind 8192 (128) 176 and 133.
     if (most < 3 || a->seqs.n_seqs < 2 || (!a->few && units * a->seqs.n_seqs >= 256)) a->prefix = 0;
+    const bool line = a->few && (over(a->seqs.max_kv, 32) + 1) * notes < (int64_t)1 << 29;    // its steps are counted in 32 bits
+    if (a->few && !line) a->prefix = 0;
     const int64_t own = a->seqs.max_kv - (a->prefix & ~31);
     const int front = a->few ? 128 : rows_of_block((int64_t)a->seqs.n_tokens * a->group, D);
     const int64_t front_units = blocks(a->seqs.n_tokens, front) * heads * halves(front);
     int64_t own_parts = 1;
     if (a->few) {
-        int64_t cut = 128;                                    // keys in a block of the line; its blocks are counted in 32 bits
-        while ((over(own, cut) + 1) * notes >= (int64_t)1 << 29) cut *= 2;
         int64_t own_blocks = kResident;
         if (a->prefix) {
             // What both cost in workgroups' time where all share the memory, in us: 64 keys for 128 rows of the front 3, 128 keys of a sequence 7 (heads of 128 in
@@ -920,13 +1063,12 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
             a->front_blocks = (int)(a->prefix_parts * front_units);
             own_blocks = std::max<int64_t>(kResident - a->front_blocks, kResident / 4);
         }
-        const int64_t longest = over(own, cut), wanted = std::max<int64_t>(own_blocks / heads + 2, 4);
+        const int64_t longest = over(own, 32), waves = 4 * own_blocks, wanted = std::max<int64_t>(waves / heads + 2, 4);
         // as many parts as one sequence of nearly all keys would be, if that is not beyond the workspace or 128 MB
         own_parts = std::min(std::min(most - a->prefix_parts, wanted), std::max<int64_t>(((int64_t)128 << 20) / per_part, 4));
-        if (own_parts >= 2) {
-            a->block_keys = (int)cut;
-            a->own_blocks = (int)own_blocks;
-            a->least_blocks = (int)std::max<int64_t>(over(longest, own_parts - 1), 1);      // a head in a stretch and part of another two, then, at most own_parts
+        if (line && own_parts >= 2) {
+            a->line_waves = (int)waves;
+            a->least_steps = (int)std::max<int64_t>(over(longest, own_parts - 1), 1);      // a head in own_parts - 1 stretches' length is in own_parts of them at most
         } else {
             own_parts = 1;
         }
@@ -955,9 +1097,9 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
 
 template <int D, int RB, bool E4M3>
 static void launch_few(const AttnArgs& a, hipStream_t stream) {
-    const int64_t own = a.block_keys ? a.own_blocks : (int64_t)a.seqs.n_seqs * a.cache.kv_heads;
-    if (a.front_blocks) attend_few_kernel<D, RB, E4M3, true><<<(unsigned)(a.front_blocks + own), 256, 0, stream>>>(a);
-    else attend_few_kernel<D, RB, E4M3, false><<<(unsigned)own, 256, 0, stream>>>(a);
+    if (a.front_blocks) attend_few_kernel<D, RB, E4M3, true><<<(unsigned)(a.front_blocks + a.line_waves / 4), 256, 0, stream>>>(a);
+    else if (a.line_waves) attend_few_kernel<D, RB, E4M3, false><<<(unsigned)(a.line_waves / 4), 256, 0, stream>>>(a);
+    else attend_rows_kernel<D, RB, E4M3><<<(unsigned)(a.seqs.n_seqs * a.cache.kv_heads), 256, 0, stream>>>(a);
 }
 
 template <int D, int NW, bool E4M3>

@@ -199,13 +199,13 @@ void patch_test_seq(int t0, int t1, int len, int n_tokens, int max_kv, int* out)
     out[0] = q.first; out[1] = q.n; out[2] = q.len; out[3] = q.pos0; out[4] = q.bad;
 }
 int patch_test_page(int id, int n_pages) { return page_or_none(id, n_pages); }
-// ... and how a call would split its keys: (prefix, own_chunk, prefix_chunk, prefix_parts, parts, bytes of the workspace, few, front_blocks, own_blocks,
-// block_keys, least_blocks); -1: refused
+// ... and how a call would split its keys: (prefix, own_chunk, prefix_chunk, prefix_parts, parts, bytes of the workspace, few, front_blocks, line_waves,
+// least_steps); -1: refused
 int patch_test_attention_plan(int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const patch_attention_opts* opts, size_t ws_bytes, int64_t* out) {
     AttnArgs a = {};
     if (fill_attention(&a, heads, seqs, cache, opts) != PATCH_OK) return -1;
     out[5] = (int64_t)plan_attention(&a, ws_bytes);
-    out[6] = a.few; out[7] = a.front_blocks; out[8] = a.own_blocks; out[9] = a.block_keys; out[10] = a.least_blocks;
+    out[6] = a.few; out[7] = a.front_blocks; out[8] = a.line_waves; out[9] = a.least_steps;
     out[0] = a.prefix; out[1] = a.own_chunk; out[2] = a.prefix_chunk; out[3] = a.prefix_parts; out[4] = a.parts;
     return 0;
 }

@@ -132,17 +132,17 @@ def test_page_numbers_out_of_range_are_none():
 def plan(H, KH, D, n_seqs, n_tokens, max_q, max_kv, prefix, ws, page=64):
     s = B.Seqs(n_seqs, n_tokens, P, P, -(-max(max_kv, 1) // page), max_q, max_kv, q_start=P)
     c = B.KVCache(P, P, 1 << 20, page, KH, D)
-    o, out = B.AttentionOpts(0.0, prefix, None, None, 0), (ctypes.c_int64 * 11)()
+    o, out = B.AttentionOpts(0.0, prefix, None, None, 0), (ctypes.c_int64 * 10)()
     assert B.lib().patch_test_attention_plan(H, s.ref, c.ref, ctypes.byref(o), ctypes.c_size_t(ws), out) == 0
     return tuple(out)
 
 
-def stretches(lens, KH, prefix, own_blocks, block_keys, least_blocks):
-    """What the workgroups of a launch for few rows take, as the kernel finds it: {(sequence, head): [(workgroup, part, first key, last key)]}."""
+def stretches(lens, KH, prefix, waves, least_steps):
+    """What the wavefronts of a launch for few rows take, as the kernel finds it: {(sequence, head): [(wavefront, part, first step, last step, steps)]}."""
     base = prefix & ~31
-    n = [-(-(L - base) // block_keys) if L > prefix else 0 for L in lens]
+    n = [-(-(L - base) // 32) if L > prefix else 0 for L in lens]
     line = [(s, h, i) for s in range(len(lens)) for h in range(KH) for i in range(n[s])]
-    stretch = max(-(-len(line) // own_blocks), least_blocks)
+    stretch = max(-(-len(line) // waves), least_steps)
     start, at = {}, 0
     for s in range(len(lens)):
         for h in range(KH):
@@ -152,7 +152,7 @@ def stretches(lens, KH, prefix, own_blocks, block_keys, least_blocks):
         me = i // stretch
         part = me - start[s, h] // stretch
         took.setdefault((s, h), {}).setdefault((me, part), []).append(b)
-    assert not line or (len(line) - 1) // stretch < own_blocks
+    assert not line or (len(line) - 1) // stretch < waves
     return {u: sorted((me, part, min(b), max(b), len(b)) for (me, part), b in t.items()) for u, t in took.items()}, n
 
 
@@ -162,22 +162,21 @@ def test_every_key_is_in_one_part_that_the_workspace_holds(H, KH, D):
                                           (2, 1, 1 << 30, 1 << 29), (1, 4096, 4096, 17), (5, 3, 0, 0), (5, 3, 40, 90), (300, 1, 300, 0), (3, 1 << 18 if H < 32 else 1 << 16, 1 << 24, 1 << 20)]:
         T = n_seqs * max_q
         for ws in (0, 15, T * H * (D + 2) * 4, 2 * T * H * (D + 2) * 4 + 16, 9 * T * H * (D + 2) * 4, 1 << 28, 1 << 62):
-            P_, own, front, front_parts, parts, used, few, front_blocks, own_blocks, block_keys, least_blocks = plan(H, KH, D, n_seqs, T, max_q, max_kv, prefix, ws)
+            P_, own, front, front_parts, parts, used, few, front_blocks, waves, least_steps = plan(H, KH, D, n_seqs, T, max_q, max_kv, prefix, ws)
             assert used <= ws and P_ in (0, min(prefix, max_kv)) and own > 0 and own % 128 == 0
             rest = max_kv - (P_ & ~31)
             if parts == 1:
-                assert P_ == 0 and own >= rest and block_keys == 0
+                assert P_ == 0 and own >= rest and waves == 0
             if P_:
                 assert front % 128 == 0 and front_parts == -(-P_ // front) >= 1
             else:
                 assert front_parts == front_blocks == 0
             if not few:
-                assert block_keys == 0 and parts - front_parts == max(1, -(-rest // own))
+                assert waves == 0 and parts - front_parts == max(1, -(-rest // own))
                 assert (parts - front_parts) * -(-max_q * H // KH // 16) <= 1 << 23
-            elif block_keys:
-                # a head of the longest sequence is in no more stretches than it has parts, wherever it begins, and the line's blocks are counted in 32 bits
-                assert own_blocks >= 1 and least_blocks * (parts - front_parts - 1) >= -(-rest // block_keys) and block_keys % 128 == 0
-                assert n_seqs * KH * (-(-rest // block_keys) + 1) < 1 << 30
+            elif waves:
+                # a head of the longest sequence is in no more stretches than it has parts, wherever it begins, and the line's steps are counted in 32 bits
+                assert waves % 4 == 0 and least_steps * (parts - front_parts - 1) >= -(-rest // 32) and n_seqs * KH * (-(-rest // 32) + 1) < 1 << 30
 
 
 @pytest.mark.parametrize("H,KH,D,max_q,prefix", [(14, 2, 64, 1, 0), (32, 32, 128, 1, 0), (32, 8, 128, 2, 1000), (8, 4, 256, 3, 500), (1, 1, 64, 1, 77)])
@@ -188,10 +187,10 @@ def test_stretches_of_ragged_batches(H, KH, D, max_q, prefix, ws):
         lens = [rng.choice([0, prefix, prefix + 1, prefix + 128, prefix + 129, rng.randrange(4000), rng.randrange(prefix, prefix + 9000)]) for _ in range(n_seqs)]
         for scale in (1.0, 1.7):                         # the caller's bound may be loose
             max_kv = int(max(max(lens), 1) * scale)
-            P_, own, front, front_parts, parts, used, few, front_blocks, own_blocks, block_keys, least_blocks = plan(H, KH, D, n_seqs, n_seqs * max_q, max_q, max_kv, prefix, ws)
-            if not (few and block_keys):
+            P_, own, front, front_parts, parts, used, few, front_blocks, waves, least_steps = plan(H, KH, D, n_seqs, n_seqs * max_q, max_q, max_kv, prefix, ws)
+            if not waves:
                 continue
-            took, n = stretches(lens, KH, P_, own_blocks, block_keys, least_blocks)
+            took, n = stretches(lens, KH, P_, waves, least_steps)
             for u, t in took.items():
                 assert [part for _, part, *_ in t] == list(range(len(t))) and len(t) <= parts - front_parts
                 assert t[0][2] == 0 and t[-1][3] == n[u[0]] - 1 and all(x[3] + 1 == y[2] for x, y in zip(t, t[1:])) and all(x[3] - x[2] + 1 == x[4] for x in t)
