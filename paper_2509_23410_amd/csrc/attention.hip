@@ -40,7 +40,7 @@ struct Span {
     int t0, rows;        // first token, rows (tokens times group)
     int pos0;            // position of token t0; in the shared front each row looks up its own
     int key0, key1;      // keys [key0, key1) are there to be read
-    int begin, end;      // and those this workgroup takes, begin a multiple of 32
+    int begin, end;      // and those this workgroup takes, begin a multiple of 64
     int part;            // its partial result, -1: it writes the result itself
     int64_t table;       // its row of the page table
     bool front, bad;
@@ -63,7 +63,7 @@ __device__ __forceinline__ Span front_span(const AttnArgs& a, int part) {
 }
 
 __device__ __forceinline__ int own_parts(const AttnArgs& a, int len) {
-    const int base = a.prefix & ~31;
+    const int base = a.prefix & ~63;
     return len > a.prefix ? (len - base + a.own_chunk - 1) / a.own_chunk : 0;
 }
 
@@ -75,7 +75,7 @@ __device__ __forceinline__ Span own_span(const AttnArgs& a, int s, const Seq& q,
     p.pos0 = q.pos0;
     p.key0 = a.prefix;
     p.key1 = max(q.len, a.prefix);
-    p.begin = (a.prefix & ~31) + chunk * a.own_chunk;
+    p.begin = (a.prefix & ~63) + chunk * a.own_chunk;
     p.end = a.line_waves ? q.len : min(q.len, p.begin + a.own_chunk);
     p.part = a.parts == 1 || (a.prefix_parts == 0 && q.len - p.begin <= a.own_chunk && chunk == 0) ? -1 : a.prefix_parts + chunk;
     p.table = s * a.seqs.table_stride;
@@ -172,11 +172,11 @@ __device__ __forceinline__ void attend_row_alone(const AttnArgs& a, const Span& 
     }
 }
 
-// Few rows: each wavefront takes steps of 32 keys of its own, K and V straight from memory into the operands' registers, RB blocks of 16 rows against
+// Few rows: each wavefront takes steps of keys of its own, K and V straight from memory into the operands' registers, RB blocks of 16 rows against
 // them; the four wavefronts' results meet in LDS.
 constexpr int kTableKeys = 4096;   // page numbers of so many keys are in LDS at a time
 
-// Page numbers of the keys [window, stop) and on to a multiple of 64 of them, -1 where there is none or it is out of range; window is a multiple of 32 and
+// Page numbers of the keys [window, stop) and on to a multiple of 64 of them, -1 where there is none or it is out of range; window is a multiple of 64 and
 // stop at most kTableKeys behind it.  Whether a key of the span is without a page.
 __device__ __forceinline__ bool load_pages(const AttnArgs& a, const Span& p, int* to, int window, int stop) {
     const int page0 = window >> a.cache.page_log2, last = window + ((stop - window + 63) & ~63) - 1, count = (last >> a.cache.page_log2) - page0 + 1;
@@ -192,62 +192,73 @@ __device__ __forceinline__ bool load_pages(const AttnArgs& a, const Span& p, int
     return none;
 }
 
-template <int D, bool E4M3>
-struct KeyRegs {
-    u32x4_t k[2][E4M3 ? D / 64 : D / 32];
-    u32x4_t v[E4M3 ? D / 32 : D / 16];
-};
+// Keys of a step: as many as fit in half a SIMD's registers beside the rows' sums.
+constexpr int step_keys(int head_dim, int blocks) { return head_dim * blocks <= 128 ? 64 : 32; }
 
-// Row i of A's tile b is key 8 (i / 4) + 4 b + i % 4 of a step: a lane then holds, of both tiles, the keys 8 g .. 8 g + 7 of its column.
-__device__ __forceinline__ int key_of_row(int row) { return 8 * (row >> 2) + (row & 3); }
+// The cells of a step, as they are loaded.  Rows of A are given out so that what a lane holds of the first product's result
+// is eight keys side by side for each 32, and the 16 (8) of both in one run: V's loads of a step then are whole rows of 64 tokens, 128 bytes together.  With
+// steps of 32 keys one sequence of 65000 keys took 59 us in pages of 32 tokens and 71 in pages of 64, whose rows were asked for in halves at different times.
+template <int D, int RB, bool E4M3>
+struct StepKeys {
+    static constexpr int kKeys = step_keys(D, RB), HB = kKeys / 32, kRun = 8 * HB;
+    static constexpr int kCell = E4M3 ? 1 : 2;
+    u32x4_t k[HB][2][E4M3 ? D / 64 : D / 32];
+    u32x4_t v[E4M3 ? HB * D / 32 : HB * D / 16];
 
-// A step's cells: k_page is the page of the lane's key in K, v_page that of its eight keys in V (both in range)
-template <int D, bool E4M3>
-__device__ __forceinline__ void load_cells(KeyRegs<D, E4M3>& r, const AttnArgs& a, int k_page, int v_page, int step, int kh, int lane) {
-    constexpr int kCell = E4M3 ? 1 : 2;
-    const int g = lane >> 4, row = lane & 15, mask = (1 << a.cache.page_log2) - 1;
-    {
-        const int at = step + key_of_row(row);
-        const PATCH_EP_GLOBAL uint8_t* base = as_global(a.cache.k) + k_page * a.cache.page_bytes + (((int64_t)kh << a.cache.page_log2) + (at & mask)) * (D * kCell) + 16 * g;
+    // the first key of the run that a lane's page numbers are of, in K and in V
+    static __device__ __forceinline__ int k_key(int lane) { return kRun * ((lane & 15) >> 2); }
+    static __device__ __forceinline__ int v_key(int lane) { return kRun * (lane >> 4); }
+
+    // page: that of the lane's run, in range
+    __device__ __forceinline__ void load_k(const AttnArgs& a, int page, int step, int kh, int lane) {
+        const int at = (step + k_key(lane) + (lane & 3)) & ((1 << a.cache.page_log2) - 1);
+        const PATCH_EP_GLOBAL uint8_t* base = as_global(a.cache.k) + page * a.cache.page_bytes + (((int64_t)kh << a.cache.page_log2) + at) * (D * kCell) + 16 * (lane >> 4);
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int h = 0; h < HB; ++h)
 #pragma unroll
-            for (int i = 0; i < (E4M3 ? D / 64 : D / 32); ++i)
-                r.k[b][i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(base + b * (4 * D * kCell) + 64 * i);
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < (E4M3 ? D / 64 : D / 32); ++i)
+                    k[h][b][i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(base + (8 * h + 4 * b) * (D * kCell) + 64 * i);
     }
-    {
-        const int at = step + 8 * g;
-        const PATCH_EP_GLOBAL uint8_t* base = as_global(a.cache.v) + v_page * a.cache.page_bytes + ((((int64_t)kh * D + row) << a.cache.page_log2) + (at & mask)) * kCell;
+    __device__ __forceinline__ void load_v(const AttnArgs& a, int page, int step, int kh, int lane) {
+        const int at = (step + v_key(lane)) & ((1 << a.cache.page_log2) - 1);
+        const PATCH_EP_GLOBAL uint8_t* base = as_global(a.cache.v) + page * a.cache.page_bytes + ((((int64_t)kh * D + (lane & 15)) << a.cache.page_log2) + at) * kCell;
         const int64_t next = (int64_t)(16 * kCell) << a.cache.page_log2;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-            if constexpr (E4M3) {
-                const u32x2_t v = *reinterpret_cast<const PATCH_EP_GLOBAL u32x2_t*>(base + i * next);
-                r.v[i / 2][2 * (i % 2)] = v[0];
-                r.v[i / 2][2 * (i % 2) + 1] = v[1];
+            if constexpr (E4M3 && HB == 2) {
+                v[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(base + i * next);
+            } else if constexpr (E4M3) {
+                const u32x2_t w = *reinterpret_cast<const PATCH_EP_GLOBAL u32x2_t*>(base + i * next);
+                v[i / 2][2 * (i % 2)] = w[0];
+                v[i / 2][2 * (i % 2) + 1] = w[1];
             } else {
-                r.v[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(base + i * next);
+#pragma unroll
+                for (int h = 0; h < HB; ++h) v[HB * i + h] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(base + i * next + 16 * h);
             }
         }
     }
-}
-template <int D, bool E4M3>
-__device__ __forceinline__ void load_keys(KeyRegs<D, E4M3>& r, const AttnArgs& a, const int* pages, int step, int kh, int lane) {
-    load_cells<D, E4M3>(r, a, max(pages[(step + key_of_row(lane & 15)) >> a.cache.page_log2], 0), max(pages[(step + 8 * (lane >> 4)) >> a.cache.page_log2], 0), step, kh, lane);
-}
-
-// the operand of 32 of a head's values (i counts them) for keys of tile b; in e4m3 a 16-byte load is the operands of two products, and Q's follow it
-template <int D, bool E4M3>
-__device__ __forceinline__ bf16x8_t key_operand(const KeyRegs<D, E4M3>& r, int b, int i) {
-    if constexpr (E4M3) return as_bf16x8(widen8(r.k[b][i / 2][2 * (i % 2)], r.k[b][i / 2][2 * (i % 2) + 1]));
-    else return as_bf16x8(r.k[b][i]);
-}
+    // operands: 32 of a head's values (i counts them) of keys of tile b of half h; eight keys of feature 16 i + column of half h
+    __device__ __forceinline__ bf16x8_t k_operand(int h, int b, int i) const {
+        if constexpr (E4M3) return as_bf16x8(widen8(k[h][b][i / 2][2 * (i % 2)], k[h][b][i / 2][2 * (i % 2) + 1]));
+        else return as_bf16x8(k[h][b][i]);
+    }
+    __device__ __forceinline__ u32x4_t v_operand(int h, int i) const {
+        if constexpr (E4M3 && HB == 2) return widen8(v[i][2 * h], v[i][2 * h + 1]);
+        else if constexpr (E4M3) return widen8(v[i / 2][2 * (i % 2)], v[i / 2][2 * (i % 2) + 1]);
+        else return v[HB * i + h];
+    }
+};
+// in e4m3 a 16-byte load of K is the operands of two products, and Q's follow it
 template <bool E4M3>
 __device__ __forceinline__ int query_offset(int i, int g) { return E4M3 ? 64 * (i / 2) + 16 * g + 8 * (i % 2) : 32 * i + 8 * g; }
 
 // What a wavefront has of its rows: running maxima (the same in all lanes of a column), sums (each lane its own keys'), and O^T.
 template <int D, int RB, bool E4M3>
 struct RowState {
+    typedef StepKeys<D, RB, E4M3> Keys;
+    static constexpr int HB = Keys::HB;
     f32x4_t o[RB][D / 16];
     float m[RB], l[RB];
 
@@ -261,37 +272,39 @@ struct RowState {
         }
     }
 
-    // A step of 32 keys; `none`: the lane's eight keys have no page.  Returns whether values that are not finite and that not every row sees went into O.
-    __device__ __forceinline__ bool step(const bf16x8_t (&q)[RB][D / 32], const KeyRegs<D, E4M3>& kv, const Span& p, int step, bool none, const int (&limit)[RB], int fewest,
-                                         float scale, int lane) {
-        const int g = lane >> 4;
-        f32x4_t s[RB][2];
+    static __device__ __forceinline__ void scores(f32x4_t (&s)[RB][HB][2], const bf16x8_t (&q)[RB][D / 32], const Keys& keys) {
 #pragma unroll
-        for (int b = 0; b < RB; ++b) s[b][0] = s[b][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int h = 0; h < HB; ++h) s[b][h][0] = s[b][h][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const bf16x8_t k = key_operand<D, E4M3>(kv, h, i);
+            for (int h = 0; h < HB; ++h)
 #pragma unroll
-                for (int b = 0; b < RB; ++b) s[b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[b][i], s[b][h], 0, 0, 0);
-            }
-        const bool ragged = step < p.key0 || step + 32 > fewest || step + 32 > p.key1 || __any(none);
-        const int key = step + 8 * g;                       // the lane's eight keys
-        bf16x8_t pr[RB];
+                for (int c = 0; c < 2; ++c) {
+                    const bf16x8_t k = keys.k_operand(h, c, i);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) s[b][h][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[b][i], s[b][h][c], 0, 0, 0);
+                }
+    }
+
+    // P of the scores, and what that does to maxima and sums.  ragged: not every row sees all the step's keys; none: the lane's have no page
+    __device__ __forceinline__ void soften(bf16x8_t (&pr)[RB][HB], const f32x4_t (&s)[RB][HB][2], const Span& p, int step, bool ragged, bool none, const int (&limit)[RB],
+                                           float scale, int lane) {
+        const int key = step + Keys::v_key(lane);
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
-            float x[8];
+            float x[HB][8], top = kNone;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = s[b][e / 4][e % 4] * scale;
-            if (ragged) {
+            for (int h = 0; h < HB; ++h)
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    x[e] = key + e >= p.key0 && key + e < limit[b] ? (none ? __builtin_nanf("") : x[e]) : kNone;
-            }
-            float top = x[0];
-#pragma unroll
-            for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+                for (int e = 0; e < 8; ++e) {
+                    x[h][e] = s[b][h][e / 4][e % 4] * scale;
+                    const int at = key + 8 * h + e;
+                    if (ragged) x[h][e] = at >= p.key0 && at < limit[b] ? (none ? __builtin_nanf("") : x[h][e]) : kNone;
+                    top = fmaxf(top, x[h][e]);
+                }
             if (__any(top > m[b] + kRise)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -301,33 +314,38 @@ struct RowState {
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) o[b][i] = o[b][i] * down;
             }
-            float sum = 0.f, y[8];
+            float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                y[e] = exp2_off(x[e], m[b]);
-                sum += y[e];
+            for (int h = 0; h < HB; ++h) {
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    y[e] = exp2_off(x[h][e], m[b]);
+                    sum += y[e];
+                }
+                pr[b][h] = as_bf16x8(u32x4_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])});
             }
             l[b] += sum;
-            pr[b] = as_bf16x8(u32x4_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])});
         }
-        u32x4_t v[D / 16];
+    }
+
+    // Returns whether values that are not finite and that not every row sees went into O.
+    __device__ __forceinline__ bool values(const bf16x8_t (&pr)[RB][HB], const Keys& keys, const Span& p, int step, bool ragged, int fewest, int lane) {
+        const int key = step + Keys::v_key(lane);
         bool infinite = false;
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-            if constexpr (E4M3) v[i] = widen8(kv.v[i / 2][2 * (i % 2)], kv.v[i / 2][2 * (i % 2) + 1]);
-            else v[i] = kv.v[i];
-            if (ragged) {                                    // cells that no key is in may hold anything, and 0 times a NaN is one
-                keep_keys(v[i], key, p.key0, p.key1);
-                infinite |= any_infinite(v[i]);
-            }
-        }
-        // ... and so may keys that only some of the rows see
-        const bool redo = ragged && fewest < min(step + 32, p.key1) && infinite;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-            for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v[i]), pr[b], o[b][i], 0, 0, 0);
-        return redo;
+            for (int h = 0; h < HB; ++h) {
+                u32x4_t v = keys.v_operand(h, i);
+                if (ragged) {                                    // cells that no key is in may hold anything, and 0 times a NaN is one
+                    keep_keys(v, key + 8 * h, p.key0, p.key1);
+                    infinite |= any_infinite(v);
+                }
+#pragma unroll
+                for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v), pr[b][h], o[b][i], 0, 0, 0);
+            }
+        return infinite && fewest < min(step + Keys::kKeys, p.key1);       // ... and so may keys that only some of the rows see
     }
 };
 
@@ -378,7 +396,7 @@ struct RowsLds {
 // All rows of a span (16 RB at most), by a workgroup of four wavefronts.
 template <int D, int RB, bool E4M3>
 __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, int kh, RowsLds<D, RB>& sh) {
-    constexpr bool kAhead = D * RB <= 128;      // with more, two steps' keys do not fit beside the rest in half a SIMD's registers
+    typedef StepKeys<D, RB, E4M3> Keys;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
     int limit[RB], fewest, most;
     row_limits<RB>(a, p, lane, limit, &fewest, &most);
@@ -397,16 +415,23 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, in
         load_pages(a, p, sh.pages, window, stop);
         __syncthreads();
         const int* pages = sh.pages - (window >> a.cache.page_log2);
-        // the keys of a wavefront's next step are on their way while it works on one; behind its last it asks for that one again
-        KeyRegs<D, E4M3> next;
-        const int first_step = window + 32 * wave, last_step = first_step + (max(stop - 1 - first_step, 0) & ~127);
-        if (kAhead && first_step < stop) load_keys<D, E4M3>(next, a, pages, first_step, kh, lane);
-        for (int step = first_step; step < stop; step += 128) {
-            KeyRegs<D, E4M3> kv = next;
-            if constexpr (kAhead) load_keys<D, E4M3>(next, a, pages, min(step + 128, last_step), kh, lane);
-            else load_keys<D, E4M3>(kv, a, pages, step, kh, lane);
-            const bool none = p.bad || pages[(step + 8 * g) >> a.cache.page_log2] < 0;
-            redo |= st.step(q, kv, p, step, none, limit, fewest, scale, lane);
+        const auto page_at = [&](int key) { return pages[key >> a.cache.page_log2]; };
+        Keys keys;
+        int step = window + Keys::kKeys * wave;
+        if (step < stop) {
+            keys.load_k(a, max(page_at(step + Keys::k_key(lane)), 0), step, kh, lane);
+            keys.load_v(a, max(page_at(step + Keys::v_key(lane)), 0), step, kh, lane);
+        }
+        for (; step < stop; step += 4 * Keys::kKeys) {           // the next K is on its way once this one is done with, and so the next V
+            const int next = step + 4 * Keys::kKeys;
+            const bool none = page_at(step + Keys::v_key(lane)) < 0, ragged = step < p.key0 || step + Keys::kKeys > fewest || step + Keys::kKeys > p.key1 || __any(none);
+            f32x4_t s[RB][Keys::HB][2];
+            bf16x8_t pr[RB][Keys::HB];
+            st.scores(s, q, keys);
+            if (next < stop) keys.load_k(a, max(page_at(next + Keys::k_key(lane)), 0), next, kh, lane);
+            st.soften(pr, s, p, step, ragged, none, limit, scale, lane);
+            redo |= st.values(pr, keys, p, step, ragged, fewest, lane);
+            if (next < stop) keys.load_v(a, max(page_at(next + Keys::v_key(lane)), 0), next, kh, lane);
         }
     }
     if (__syncthreads_or(redo)) {
@@ -760,7 +785,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttnArgs a) {
     if (p.rows > 0) attend_rows<D, RB, E4M3>(a, p, blockIdx.x % a.cache.kv_heads, sh);
 }
 
-// A step of the line of all sequences' own keys: sequence by sequence, in it head by head, in that 32 keys at a time.
+// A step of the line of all sequences' own keys: sequence by sequence, in it head by head, in that so many keys at a time.
 struct Place {
     Seq q;
     int s, kh, n, i, unit;      // sequence, key head, steps of a head of it, which of them this is, and the line's number of the head's first
@@ -770,9 +795,10 @@ struct Place {
 // behind that are on their way while it works on one, and what it has of a head's rows it writes when that head or its stretch ends.
 template <int D, int RB, bool E4M3>
 __device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
-    constexpr bool kAhead = D * RB <= 128;
-    const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15, KH = a.cache.kv_heads, base = a.prefix & ~31;
-    const auto steps_in = [&](const Seq& q) { return q.n > 0 && q.len > a.prefix ? (q.len - base + 31) / 32 : 0; };
+    typedef StepKeys<D, RB, E4M3> Keys;
+    constexpr int kKeys = Keys::kKeys;
+    const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15, KH = a.cache.kv_heads, base = a.prefix & ~63;
+    const auto steps_in = [&](const Seq& q) { return q.n > 0 && q.len > a.prefix ? (q.len - base + kKeys - 1) / kKeys : 0; };
     // steps of 64 sequences from s0 on, one a lane, and their sums up to each
     const auto sums_of = [&](int s0, int* upto) {
         const int n = s0 + lane < a.seqs.n_seqs ? steps_in(seq_at(a.seqs, s0 + lane)) : 0;
@@ -837,9 +863,9 @@ __device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
             p.n = steps_in(p.q);
         } while (p.n == 0 && p.s < a.seqs.n_seqs - 1);
     };
-    // pages of the lane's key in K and of its keys in V: -1 where there is none
+    // pages of the lane's runs of keys in K and in V: -1 where there is none
     const auto ask_pages = [&](const Place& p, int* k_page, int* v_page) {
-        const int k_key = base + 32 * p.i + key_of_row(col), v_key = base + 32 * p.i + 8 * g;
+        const int k_key = base + kKeys * p.i + Keys::k_key(lane), v_key = base + kKeys * p.i + Keys::v_key(lane);
         const PATCH_EP_GLOBAL int32_t* row = as_global(a.seqs.table) + p.s * a.seqs.table_stride;
         *k_page = *v_page = -1;
         if (k_key < p.q.len) *k_page = row[k_key >> a.cache.page_log2];
@@ -861,7 +887,7 @@ __device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
     bool redo = false;
     // Loads come back in the order in which they were asked for: the page numbers of a step are asked for in front of the cells of the step before it, so that
     // the wait for them is none for those.
-    KeyRegs<D, E4M3> next;
+    Keys keys;
     Place f = c;
     if (count > 1) go_on(f);
     int k_now, v_now, k_id, v_id;
@@ -869,9 +895,10 @@ __device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
     ask_pages(f, &k_id, &v_id);
     k_now = checked(c, k_now);
     v_now = checked(c, v_now);
-    if constexpr (kAhead) load_cells<D, E4M3>(next, a, max(k_now, 0), max(v_now, 0), base + 32 * c.i, c.kh, lane);
+    keys.load_k(a, max(k_now, 0), base + kKeys * c.i, c.kh, lane);
+    keys.load_v(a, max(v_now, 0), base + kKeys * c.i, c.kh, lane);
     for (int t = 0; t < count; ++t) {
-        const int step = base + 32 * c.i;
+        const int step = base + kKeys * c.i;
         if (t == 0 || c.i == 0) {                                 // a head's rows
             p = own_span(a, c.s, c.q, 0);
             p.begin = step;
@@ -883,22 +910,26 @@ __device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
             st.clear();
             redo = false;
         }
-        KeyRegs<D, E4M3> kv = next;
-        const bool none = v_now < 0;
-        if constexpr (!kAhead) load_cells<D, E4M3>(kv, a, max(k_now, 0), max(v_now, 0), step, c.kh, lane);
+        const bool none = v_now < 0, more = t + 1 < count;
+        const int fewest = p.pos0 + 1;
+        const bool ragged = step < p.key0 || step + kKeys > fewest || __any(none);       // (a row sees nothing that is not there)
+        f32x4_t s[RB][Keys::HB][2];
+        bf16x8_t pr[RB][Keys::HB];
+        st.scores(s, q, keys);
         k_now = checked(f, k_id);
         v_now = checked(f, v_id);
         Place ff = f;
         if (t + 2 < count) go_on(ff);
         ask_pages(ff, &k_id, &v_id);
-        if constexpr (kAhead) load_cells<D, E4M3>(next, a, max(k_now, 0), max(v_now, 0), base + 32 * f.i, f.kh, lane);
-
-        redo |= st.step(q, kv, p, step, none, limit, p.pos0 + 1, scale, lane);
+        if (more) keys.load_k(a, max(k_now, 0), base + kKeys * f.i, f.kh, lane);
+        st.soften(pr, s, p, step, ragged, none, limit, scale, lane);
+        redo |= st.values(pr, keys, p, step, ragged, fewest, lane);
+        if (more) keys.load_v(a, max(v_now, 0), base + kKeys * f.i, f.kh, lane);
 
         const bool ends = c.i == c.n - 1;
         if (ends || t == count - 1) {
             const int part = me - c.unit / stretch;
-            p.end = min(p.end, step + 32);
+            p.end = min(p.end, step + kKeys);
             p.part = a.prefix_parts == 0 && ends && c.i <= t ? -1 : a.prefix_parts + part;      // all of the head's keys: the result itself
             if (ends && lane == 0) as_global_out(a.unit_parts)[c.s * KH + c.kh] = part + 1;
             if (__any(redo)) {
@@ -1045,7 +1076,7 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     if (most < 3 || a->seqs.n_seqs < 2 || (!a->few && units * a->seqs.n_seqs >= 256)) a->prefix = 0;
     const bool line = a->few && (over(a->seqs.max_kv, 32) + 1) * notes < (int64_t)1 << 29;    // its steps are counted in 32 bits
     if (a->few && !line) a->prefix = 0;
-    const int64_t own = a->seqs.max_kv - (a->prefix & ~31);
+    const int64_t own = a->seqs.max_kv - (a->prefix & ~63);
     const int front = a->few ? 128 : rows_of_block((int64_t)a->seqs.n_tokens * a->group, D);
     const int64_t front_units = blocks(a->seqs.n_tokens, front) * heads * halves(front);
     int64_t own_parts = 1;
@@ -1063,7 +1094,7 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
             a->front_blocks = (int)(a->prefix_parts * front_units);
             own_blocks = std::max<int64_t>(kResident - a->front_blocks, kResident / 4);
         }
-        const int64_t longest = over(own, 32), waves = 4 * own_blocks, wanted = std::max<int64_t>(waves / heads + 2, 4);
+        const int64_t longest = over(own, step_keys(D, block / 16)), waves = 4 * own_blocks, wanted = std::max<int64_t>(waves / heads + 2, 4);
         // as many parts as one sequence of nearly all keys would be, if that is not beyond the workspace or 128 MB
         own_parts = std::min(std::min(most - a->prefix_parts, wanted), std::max<int64_t>(((int64_t)128 << 20) / per_part, 4));
         if (line && own_parts >= 2) {

@@ -137,10 +137,10 @@ def plan(H, KH, D, n_seqs, n_tokens, max_q, max_kv, prefix, ws, page=64):
     return tuple(out)
 
 
-def stretches(lens, KH, prefix, waves, least_steps):
+def stretches(lens, KH, prefix, waves, least_steps, step):
     """What the wavefronts of a launch for few rows take, as the kernel finds it: {(sequence, head): [(wavefront, part, first step, last step, steps)]}."""
-    base = prefix & ~31
-    n = [-(-(L - base) // 32) if L > prefix else 0 for L in lens]
+    base = prefix & ~63
+    n = [-(-(L - base) // step) if L > prefix else 0 for L in lens]
     line = [(s, h, i) for s in range(len(lens)) for h in range(KH) for i in range(n[s])]
     stretch = max(-(-len(line) // waves), least_steps)
     start, at = {}, 0
@@ -164,7 +164,7 @@ def test_every_key_is_in_one_part_that_the_workspace_holds(H, KH, D):
         for ws in (0, 15, T * H * (D + 2) * 4, 2 * T * H * (D + 2) * 4 + 16, 9 * T * H * (D + 2) * 4, 1 << 28, 1 << 62):
             P_, own, front, front_parts, parts, used, few, front_blocks, waves, least_steps = plan(H, KH, D, n_seqs, T, max_q, max_kv, prefix, ws)
             assert used <= ws and P_ in (0, min(prefix, max_kv)) and own > 0 and own % 128 == 0
-            rest = max_kv - (P_ & ~31)
+            rest, step = max_kv - (P_ & ~63), 64 if D * (1 if max_q * H // KH <= 16 else 2) <= 128 else 32
             if parts == 1:
                 assert P_ == 0 and own >= rest and waves == 0
             if P_:
@@ -176,7 +176,7 @@ def test_every_key_is_in_one_part_that_the_workspace_holds(H, KH, D):
                 assert (parts - front_parts) * -(-max_q * H // KH // 16) <= 1 << 23
             elif waves:
                 # a head of the longest sequence is in no more stretches than it has parts, wherever it begins, and the line's steps are counted in 32 bits
-                assert waves % 4 == 0 and least_steps * (parts - front_parts - 1) >= -(-rest // 32) and n_seqs * KH * (-(-rest // 32) + 1) < 1 << 30
+                assert waves % 4 == 0 and least_steps * (parts - front_parts - 1) >= -(-rest // step) and n_seqs * KH * (-(-rest // step) + 1) < 1 << 30
 
 
 @pytest.mark.parametrize("H,KH,D,max_q,prefix", [(14, 2, 64, 1, 0), (32, 32, 128, 1, 0), (32, 8, 128, 2, 1000), (8, 4, 256, 3, 500), (1, 1, 64, 1, 77)])
@@ -190,7 +190,7 @@ def test_stretches_of_ragged_batches(H, KH, D, max_q, prefix, ws):
             P_, own, front, front_parts, parts, used, few, front_blocks, waves, least_steps = plan(H, KH, D, n_seqs, n_seqs * max_q, max_q, max_kv, prefix, ws)
             if not waves:
                 continue
-            took, n = stretches(lens, KH, P_, waves, least_steps)
+            took, n = stretches(lens, KH, P_, waves, least_steps, 64 if D * (1 if max_q * H // KH <= 16 else 2) <= 128 else 32)
             for u, t in took.items():
                 assert [part for _, part, *_ in t] == list(range(len(t))) and len(t) <= parts - front_parts
                 assert t[0][2] == 0 and t[-1][3] == n[u[0]] - 1 and all(x[3] + 1 == y[2] for x, y in zip(t, t[1:])) and all(x[3] - x[2] + 1 == x[4] for x in t)
