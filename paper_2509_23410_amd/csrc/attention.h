@@ -59,7 +59,7 @@ struct AttnArgs {
     int prefix_chunk, prefix_parts;
     int parts;                // prefix_parts + the most that a sequence's own keys are; 1: workgroups write O, else partial results
     // few rows a sequence: one launch of front_blocks workgroups for the shared front and line_waves wavefronts that have equal stretches (least_steps at least)
-    // of all own keys, in steps of 64 keys, or 32 for the larger blocks; 0: a workgroup for each sequence and key head
+    // of all own keys, in steps of 64 keys (heads of 256: 32); 0: a workgroup for each sequence and key head
     int few, front_blocks, line_waves, least_steps;
     float* part_ml;           // parts x n_tokens x heads pairs: running maximum (of scores times log2(e)) and sum
     float* part_o;            // parts x n_tokens x heads x head_dim

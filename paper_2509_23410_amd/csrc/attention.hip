@@ -92,11 +92,15 @@ __device__ __forceinline__ int row_limit(const AttnArgs& a, const Span& p, int r
     return t - q.first < q.n ? min(a.prefix, q.pos0 + t - q.first + 1) : 0;
 }
 
-// Of a lane's eight keys from `key` on, zero where they are not in [lo, hi).
-__device__ __forceinline__ void keep_keys(u32x4_t& v, int key, int lo, int hi) {
+// Bits of eight keys' cells from `key` on: ones for those that are in [lo, hi).
+__device__ __forceinline__ u32x4_t keys_in(int key, int lo, int hi) {
+    u32x4_t bits;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (key + e < lo || key + e >= hi) v[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
+    for (int e = 0; e < 4; ++e) {
+        const int at = key + 2 * e;
+        bits[e] = (at >= lo && at < hi ? 0x0000FFFFu : 0u) | (at + 1 >= lo && at + 1 < hi ? 0xFFFF0000u : 0u);
+    }
+    return bits;
 }
 __device__ __forceinline__ bool any_infinite(const u32x4_t& v) {      // or NaN
     bool any = false;
@@ -192,15 +196,18 @@ __device__ __forceinline__ bool load_pages(const AttnArgs& a, const Span& p, int
     return none;
 }
 
-// Keys of a step: as many as fit in half a SIMD's registers beside the rows' sums.
-constexpr int step_keys(int head_dim, int blocks) { return head_dim * blocks <= 128 ? 64 : 32; }
+// Keys of a step, and workgroups of four wavefronts on a compute unit: with wider heads or more rows a wavefront has its SIMD, and all of its registers, to
+// itself.  32 sequences of 2000 keys and 5 tokens of 4 query heads (blocks of 32 rows): 64 keys with a SIMD to itself 67.7 us, 32 72.2, 32 by two 77.3; of 8000
+// keys with one head of 256: 91.7 (spilled registers), 58.4, 92.3.
+constexpr int step_keys(int head_dim) { return head_dim == 256 ? 32 : 64; }
+constexpr int rows_resident(int head_dim, int blocks) { return head_dim * blocks <= 128 ? 2 : 1; }
 
 // The cells of a step, as they are loaded.  Rows of A are given out so that what a lane holds of the first product's result
 // is eight keys side by side for each 32, and the 16 (8) of both in one run: V's loads of a step then are whole rows of 64 tokens, 128 bytes together.  With
 // steps of 32 keys one sequence of 65000 keys took 59 us in pages of 32 tokens and 71 in pages of 64, whose rows were asked for in halves at different times.
 template <int D, int RB, bool E4M3>
 struct StepKeys {
-    static constexpr int kKeys = step_keys(D, RB), HB = kKeys / 32, kRun = 8 * HB;
+    static constexpr int kKeys = step_keys(D), HB = kKeys / 32, kRun = 8 * HB;
     static constexpr int kCell = E4M3 ? 1 : 2;
     u32x4_t k[HB][2][E4M3 ? D / 64 : D / 32];
     u32x4_t v[E4M3 ? HB * D / 32 : HB * D / 16];
@@ -332,20 +339,24 @@ struct RowState {
     // Returns whether values that are not finite and that not every row sees went into O.
     __device__ __forceinline__ bool values(const bf16x8_t (&pr)[RB][HB], const Keys& keys, const Span& p, int step, bool ragged, int fewest, int lane) {
         const int key = step + Keys::v_key(lane);
+        // cells that no key is in may hold anything, and 0 times a NaN is one; and so may keys that only some of the rows see
+        const bool some = fewest < min(step + Keys::kKeys, p.key1);
         bool infinite = false;
+        u32x4_t bits[HB];
+        if (ragged)
+#pragma unroll
+            for (int h = 0; h < HB; ++h) bits[h] = keys_in(key + 8 * h, p.key0, p.key1);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
             for (int h = 0; h < HB; ++h) {
                 u32x4_t v = keys.v_operand(h, i);
-                if (ragged) {                                    // cells that no key is in may hold anything, and 0 times a NaN is one
-                    keep_keys(v, key + 8 * h, p.key0, p.key1);
-                    infinite |= any_infinite(v);
-                }
+                if (ragged) v &= bits[h];
+                if (some) infinite |= any_infinite(v);
 #pragma unroll
                 for (int b = 0; b < RB; ++b) o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v), pr[b][h], o[b][i], 0, 0, 0);
             }
-        return infinite && fewest < min(step + Keys::kKeys, p.key1);       // ... and so may keys that only some of the rows see
+        return infinite;
     }
 };
 
@@ -621,7 +632,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
                     u32x4_t v = v_regs[i];
                     if constexpr (E4M3) v = widen8(v_regs[i][2 * b], v_regs[i][2 * b + 1]);
                     if (any_none && v_none) v = u32x4_t{0, 0, 0, 0};
-                    if (edge) keep_keys(v, tile + v_key + 8 * b, p.key0, p.key1);        // cells that no key is in
+                    if (edge) v &= keys_in(tile + v_key + 8 * b, p.key0, p.key1);        // cells that no key is in
                     if (!seen_by_all) infinite |= any_infinite(v);
                     sh.v[buffer][chunk_at<kTile / 8>(v_row + i * kFeatureStep, v_key / 8 + b)] = v;
                 }
@@ -778,7 +789,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tiles_kernel(const AttnArgs
 
 // Few rows a sequence and nowhere to put parts: a workgroup for each sequence and key head.
 template <int D, int RB, bool E4M3>
-__global__ __launch_bounds__(256, 2) void attend_rows_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, rows_resident(D, RB)) void attend_rows_kernel(const AttnArgs a) {
     __shared__ RowsLds<D, RB> sh;
     const int s = blockIdx.x / a.cache.kv_heads;
     const Span p = own_span(a, s, seq_at(a.seqs, s), 0);
@@ -800,8 +811,9 @@ __device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15, KH = a.cache.kv_heads, base = a.prefix & ~63;
     const auto steps_in = [&](const Seq& q) { return q.n > 0 && q.len > a.prefix ? (q.len - base + kKeys - 1) / kKeys : 0; };
     // steps of 64 sequences from s0 on, one a lane, and their sums up to each
-    const auto sums_of = [&](int s0, int* upto) {
-        const int n = s0 + lane < a.seqs.n_seqs ? steps_in(seq_at(a.seqs, s0 + lane)) : 0;
+    const auto sums_of = [&](int s0, Seq* q, int* upto) {
+        *q = seq_at(a.seqs, min(s0 + lane, a.seqs.n_seqs - 1));
+        const int n = s0 + lane < a.seqs.n_seqs ? steps_in(*q) : 0;
         int sum = n;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
@@ -813,16 +825,19 @@ __device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
     };
     Place c;
     c.s = c.unit = 0;
-    c.q = seq_at(a.seqs, 0);
+    if (a.seqs.n_seqs == 1) c.q = seq_at(a.seqs, 0);
+    else c.q = Seq{};
     int total, n0 = 0, upto0 = 0;
+    Seq q0 = c.q;
     if (a.seqs.n_seqs == 1) {
         total = steps_in(c.q) * KH;
     } else {
-        n0 = sums_of(0, &upto0);
+        n0 = sums_of(0, &q0, &upto0);
         total = __builtin_amdgcn_readlane(upto0, 63);
         for (int s0 = 64; s0 < a.seqs.n_seqs; s0 += 64) {
+            Seq unused;
             int upto;
-            sums_of(s0, &upto);
+            sums_of(s0, &unused, &upto);
             total += __builtin_amdgcn_readlane(upto, 63);
         }
         total *= KH;
@@ -837,12 +852,16 @@ __device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
                 const int which = __builtin_ctzll(there);
                 c.s = s0 + which;
                 c.unit = before + KH * (__builtin_amdgcn_readlane(upto0, which) - __builtin_amdgcn_readlane(n0, which));
+                c.q.first = __builtin_amdgcn_readlane(q0.first, which);
+                c.q.n = __builtin_amdgcn_readlane(q0.n, which);
+                c.q.len = __builtin_amdgcn_readlane(q0.len, which);
+                c.q.pos0 = c.q.len - c.q.n;
+                c.q.bad = __builtin_amdgcn_readlane((int)q0.bad, which);
                 break;
             }
             before += KH * __builtin_amdgcn_readlane(upto0, 63);
-            n0 = sums_of(s0 + 64, &upto0);
+            n0 = sums_of(s0 + 64, &q0, &upto0);
         }
-        c.q = seq_at(a.seqs, c.s);
     }
     c.n = steps_in(c.q);
     if (c.n == 0) return;                                         // (there is one: total is not 0)
@@ -977,7 +996,7 @@ __device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
 // with the others, and the work of a compute unit is bounded by nothing but what its memory can bring.  A sequence's head that lies in several stretches is
 // as many parts; who has its last step notes how many.
 template <int D, int RB, bool E4M3, bool FRONT>
-__global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(256, rows_resident(D, RB)) void attend_few_kernel(const AttnArgs a) {
     if constexpr (FRONT) {
         __shared__ TilesLds<D, 4> sh;
         constexpr int kHalves = D / TilesLds<D, 4>::DV;
@@ -1048,7 +1067,7 @@ static int rows_of_block(int64_t rows, int head_dim) {
 static inline int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 static inline int64_t over(int64_t x, int64_t m) { return (x + m - 1) / m; }
 
-constexpr int64_t kResident = 512;                            // workgroups of four wavefronts, two on each compute unit, that are there at once
+constexpr int64_t kResident = 512;                            // workgroups of four wavefronts that are there at once: two on each compute unit
 constexpr int64_t kMostGroups = (int64_t)1 << 22;             // workgroups in x: far from the 2^32 threads that one launch may have there
 
 // Keys that a workgroup takes, so that a launch over `keys` of them for `units` sequences, key heads and blocks of 128 rows or more fills the chip once.
@@ -1081,20 +1100,21 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     const int64_t front_units = blocks(a->seqs.n_tokens, front) * heads * halves(front);
     int64_t own_parts = 1;
     if (a->few) {
-        int64_t own_blocks = kResident;
+        const int64_t resident = kResident / 2 * rows_resident(D, block / 16);
+        int64_t own_blocks = resident;
         if (a->prefix) {
             // What both cost in workgroups' time where all share the memory, in us: 64 keys for 128 rows of the front 3, 128 keys of a sequence 7 (heads of 128 in
             // bf16); the longest sequence is known, and the others are taken to be half as long on the whole.
             const double f = 3.0 * front_units * over(a->prefix, 64), o = (a->cache.e4m3 ? 3.5 : 7.0) * 0.5 * notes * over(std::max<int64_t>(own, 1), 128);
-            const int64_t share = (int64_t)(kResident * f / (f + o));
+            const int64_t share = (int64_t)(resident * f / (f + o));
             int64_t parts = std::max<int64_t>(over(share, front_units), 1);
             parts = std::min(std::min(parts, over(a->prefix, 128)), std::min(most - 2, std::max<int64_t>(kMostGroups / front_units, 1)));
             a->prefix_chunk = (int)up_to(over(a->prefix, parts), 128);
             a->prefix_parts = (int)over(a->prefix, a->prefix_chunk);
             a->front_blocks = (int)(a->prefix_parts * front_units);
-            own_blocks = std::max<int64_t>(kResident - a->front_blocks, kResident / 4);
+            own_blocks = std::max<int64_t>(resident - a->front_blocks, resident / 4);
         }
-        const int64_t longest = over(own, step_keys(D, block / 16)), waves = 4 * own_blocks, wanted = std::max<int64_t>(waves / heads + 2, 4);
+        const int64_t longest = over(own, step_keys(D)), waves = 4 * own_blocks, wanted = std::max<int64_t>(waves / heads + 2, 4);
         // as many parts as one sequence of nearly all keys would be, if that is not beyond the workspace or 128 MB
         own_parts = std::min(std::min(most - a->prefix_parts, wanted), std::max<int64_t>(((int64_t)128 << 20) / per_part, 4));
         if (line && own_parts >= 2) {

@@ -164,7 +164,7 @@ def test_every_key_is_in_one_part_that_the_workspace_holds(H, KH, D):
         for ws in (0, 15, T * H * (D + 2) * 4, 2 * T * H * (D + 2) * 4 + 16, 9 * T * H * (D + 2) * 4, 1 << 28, 1 << 62):
             P_, own, front, front_parts, parts, used, few, front_blocks, waves, least_steps = plan(H, KH, D, n_seqs, T, max_q, max_kv, prefix, ws)
             assert used <= ws and P_ in (0, min(prefix, max_kv)) and own > 0 and own % 128 == 0
-            rest, step = max_kv - (P_ & ~63), 64 if D * (1 if max_q * H // KH <= 16 else 2) <= 128 else 32
+            rest, step = max_kv - (P_ & ~63), 32 if D == 256 else 64
             if parts == 1:
                 assert P_ == 0 and own >= rest and waves == 0
             if P_:
@@ -190,7 +190,7 @@ def test_stretches_of_ragged_batches(H, KH, D, max_q, prefix, ws):
             P_, own, front, front_parts, parts, used, few, front_blocks, waves, least_steps = plan(H, KH, D, n_seqs, n_seqs * max_q, max_q, max_kv, prefix, ws)
             if not waves:
                 continue
-            took, n = stretches(lens, KH, P_, waves, least_steps, 64 if D * (1 if max_q * H // KH <= 16 else 2) <= 128 else 32)
+            took, n = stretches(lens, KH, P_, waves, least_steps, 32 if D == 256 else 64)
             for u, t in took.items():
                 assert [part for _, part, *_ in t] == list(range(len(t))) and len(t) <= parts - front_parts
                 assert t[0][2] == 0 and t[-1][3] == n[u[0]] - 1 and all(x[3] + 1 == y[2] for x, y in zip(t, t[1:])) and all(x[3] - x[2] + 1 == x[4] for x in t)
