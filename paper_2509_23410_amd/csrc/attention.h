@@ -54,7 +54,7 @@ struct AttnArgs {
     CacheArgs cache;
     int heads, group;         // query heads, and how many of them share a key head
     float scale;              // times log2(e)
-    int prefix;               // keys [0, prefix) are those of the first sequence's row for all; they take parts of their own
+    int prefix;               // keys [0, prefix) are the same for all: they take parts of their own
     int own_chunk;            // keys of a sequence's own that one workgroup takes: a multiple of 128, counted from prefix rounded down to 64
     int prefix_chunk, prefix_parts;
     int parts;                // prefix_parts + the most that a sequence's own keys are; 1: workgroups write O, else partial results

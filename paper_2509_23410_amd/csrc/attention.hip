@@ -35,7 +35,7 @@ constexpr float kRise = 8.f;
 // exp2(x - m) where m may be the maximum of nothing
 __device__ __forceinline__ float exp2_off(float x, float m) { return __builtin_amdgcn_exp2f(x - (m == kNone ? 0.f : m)); }
 
-// Which rows and keys a workgroup has.  The shared front is one batch of all tokens against the first sequence's pages.
+// Which rows and keys a workgroup has.  The shared front is one batch of all tokens against the pages of one sequence.
 struct Span {
     int t0, rows;        // first token, rows (tokens times group)
     int pos0;            // position of token t0; in the shared front each row looks up its own
@@ -57,8 +57,19 @@ __device__ __forceinline__ Span front_span(const AttnArgs& a, int part) {
     p.begin = part * a.prefix_chunk;
     p.end = min(a.prefix, p.begin + a.prefix_chunk);
     p.part = part;
-    p.table = 0;
     p.bad = false;
+    // the pages are those in the row of the first sequence that has them all: one of padding may be in front of it
+    int s = 0;
+    const int lane = threadIdx.x & 63;
+    for (int s0 = 0; s0 < a.seqs.n_seqs; s0 += 64) {
+        const int len = as_global(a.seqs.kv_len)[min(s0 + lane, a.seqs.n_seqs - 1)];
+        const uint64_t there = __ballot(s0 + lane < a.seqs.n_seqs && len >= a.prefix && len <= a.seqs.max_kv);
+        if (there) {
+            s = s0 + __builtin_ctzll(there);
+            break;
+        }
+    }
+    p.table = __builtin_amdgcn_readfirstlane(s) * a.seqs.table_stride;
     return p;
 }
 
@@ -559,16 +570,18 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
     const int end = p.front ? p.end : min(p.end, p.pos0 + min(first_row + 32 * NW - 1, p.rows - 1) / a.group + 1);
 
     const int64_t q_at = there ? (int64_t)(p.t0 + r / a.group) * a.q_stride + (int64_t)(kh * a.group + r % a.group) * D : 0;
+    float scale = a.scale;
+    if (E4M3 && a.cache.k_scale) scale *= as_global(a.cache.k_scale)[kh];
     bf16x8_t q[D / 16];
-    const uint32_t turn = a.scale < 0.f ? 0x80008000u : 0u;                    // so that the largest product is the largest score
+    const uint32_t turn = scale < 0.f ? 0x80008000u : 0u;                      // so that the largest product is the largest score
+    if (scale < 0.f) scale = -scale;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
         u32x4_t v = {0, 0, 0, 0};
         if (there) v = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(a.Q) + q_at + 16 * i + 8 * h) ^ turn;
         q[i] = as_bf16x8(v);
     }
-    float scale = a.scale < 0.f ? -a.scale : a.scale;
-    if (E4M3 && a.cache.k_scale) scale *= as_global(a.cache.k_scale)[kh];
+    if (scale == 0.f) scale = 1.17549435e-38f;                                 // (a masked score, minus infinity, has to stay that)
 
     f32x16_t o[DV / 32];
 #pragma unroll
@@ -698,7 +711,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
             float top = s[0][0];
 #pragma unroll
             for (int e = 1; e < kTile / 2; ++e) top = fmaxf(top, s[e / 16][e % 16]);
-            top = top == kNone ? kNone : top * scale;                          // (a scale of zero makes no NaN of it)
+            top *= scale;
             if (__any(top > m + kRise)) {
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float m_new = fmaxf(m, top), down = exp2_off(m, m_new);
@@ -1021,7 +1034,7 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const AttnArgs a) {
     const int t = blockIdx.x, head = blockIdx.y;
     const int seq = seq_of(a.seqs, t);
     const Seq q = seq_at(a.seqs, seq);
-    if (t - q.first >= q.n) return;                           // no sequence has this token
+    if (t - q.first >= q.n || t - q.first >= a.seqs.max_q) return;     // no sequence has this token, or it is one too many
     const int own = !a.line_waves ? own_parts(a, q.len) : q.len <= a.prefix ? 0 : as_global(a.unit_parts)[seq * a.cache.kv_heads + head / a.group];
     if (a.prefix_parts == 0 && (own == 1 || (own == 0 && !a.line_waves))) return;     // written by the workgroup itself
     const int parts = a.prefix_parts + own;

@@ -374,3 +374,27 @@ def test_pages_beyond_4_gb():
     torch.cuda.synchronize()
     last = k[where[b.table[0, 3]]].view(KH, page, D)
     assert torch.equal(last[:, 199 % page], x[2].view(KH, D)) and torch.equal(v[where[b.table[1, 1]]].view(KH, D, page)[:, :, 69 % page], x[3].view(KH, D))
+
+
+def test_scales_of_any_kind():
+    """Heads whose keys' scale is zero or negative, and one whose values' is."""
+    for n, kv in (([1, 1], [300, 77]), ([90], [120])):
+        b = R.Batch(n, kv, 4, 128, 16, e4m3=True, seed=21)
+        raw_k, raw_v = [x / b.k_scale.double()[:, None] for x in b.ks], [x / b.v_scale.double()[:, None] for x in b.vs]
+        b.k_scale[1], b.k_scale[2], b.v_scale[3] = 0.0, -b.k_scale[2], -b.v_scale[3]
+        b.ks, b.vs = [x * b.k_scale.double()[:, None] for x in raw_k], [x * b.v_scale.double()[:, None] for x in raw_v]
+        Q, O, lse = _run(b, 8)
+        _check(b, Q, 8, O, lse)
+
+
+def test_more_sequences_than_a_wavefront_has_lanes():
+    """Empty ones, ones without new tokens, short and long, in the order of nothing; with a shared front and without."""
+    kv = [(37 * i) % 400 if i % 5 else 0 for i in range(200)]
+    n = [0 if i % 7 == 3 else 1 + (i % 3 == 1) for i in range(200)]
+    for prefix in (0, 70):
+        lens = [L if L == 0 else L + prefix for L in kv]
+        b = R.Batch(n, lens, 2, 64, 32, prefix=prefix, seed=22)
+        for workspace in ("all", "half", "none"):
+            # rows of sequences of nothing see nothing of the shared front, either
+            Q, O, lse = _run(b, 6, workspace=workspace)
+            _check(b, Q, 6, O, lse)
