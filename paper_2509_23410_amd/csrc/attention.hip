@@ -680,6 +680,9 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
             ask_keys(tile + kTile);
         }
         if (tile < most) {
+            // ahead of a wavefront that is in its softmax: the matrix instructions of one then lie under the rest of the other.  A prompt of 4096 over 32 heads of
+            // 128, both on one card: 185.8 us, and 175.2 so.
+            __builtin_amdgcn_s_setprio(1);
             f32x16_t s[kBlocks];
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
@@ -698,6 +701,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
                 __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
             __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
+            __builtin_amdgcn_s_setprio(0);
             const bool ragged = tile < p.key0 || tile + kTile > fewest;
             if (ragged) {
 #pragma unroll
