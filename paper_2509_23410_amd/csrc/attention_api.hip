@@ -199,6 +199,13 @@ void patch_test_seq(int t0, int t1, int len, int n_tokens, int max_kv, int* out)
     out[0] = q.first; out[1] = q.n; out[2] = q.len; out[3] = q.pos0; out[4] = q.bad;
 }
 int patch_test_page(int id, int n_pages) { return page_or_none(id, n_pages); }
+// ... a tile of new positions: whether there are any in it, its bounds, and the row that each of its positions is read from
+void patch_test_new_tile(int t0, int t1, int len, int n_tokens, int max_kv, int tile, int* out) {
+    const Seq q = seq_from(t0, t1, len, n_tokens, max_kv);
+    const NewTile n = new_tile(q, tile);
+    out[0] = !n.none; out[1] = n.begin; out[2] = n.base;
+    for (int i = 0; i < kTurn; ++i) out[3 + i] = row_of_new(q, n, i);
+}
 // ... and how a call would split its keys: (prefix, own_chunk, prefix_chunk, prefix_parts, parts, bytes of the workspace, few, front_blocks, line_waves,
 // least_steps); -1: refused
 int patch_test_attention_plan(int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const patch_attention_opts* opts, size_t ws_bytes, int64_t* out) {

@@ -11,15 +11,13 @@ namespace patch {
 
 // V of a tile of 64 positions of one sequence and key head, turned in LDS: a feature's tokens side by side, as the page holds them.  By itself each value is a
 // store of its own, a page's tokens apart: two prompts of 1100 tokens, 32 key heads of 128, e4m3, 70.3 us, in tiles 37.9.
-constexpr int kTurn = 64;
-
 template <int D>
 __device__ __forceinline__ void append_v_tile(const RopeArgs& a, int tile, int kh, int s) {
     __shared__ uint16_t sh_v[D][kTurn + 2];                      // bf16, or e4m3 in the low byte; rows an odd number of words apart
     const Seq q = seq_at(a.seqs, s);
-    if (q.bad) return;
-    const int begin = max(q.pos0, 0), base = (begin & ~(kTurn - 1)) + tile * kTurn;      // its new tokens have positions begin .. q.len - 1
-    if (base >= q.len) return;
+    const NewTile there = new_tile(q, tile);
+    if (there.none) return;
+    const int begin = there.begin, base = there.base;
     const float scale = a.cache.v_scale ? as_global(a.cache.v_scale)[kh] : 1.f;
     constexpr int kThreads = D / 4;
     const int d = (threadIdx.x % kThreads) * 4, i0 = threadIdx.x / kThreads;
@@ -27,7 +25,7 @@ __device__ __forceinline__ void append_v_tile(const RopeArgs& a, int tile, int k
     Four x[kLoads];
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {                           // all asked for together; a position that is not new has another's value, which is not stored
-        const int64_t t = q.first + (within(base + i0 + n * kStep, begin, q.len - 1) - q.pos0);
+        const int64_t t = row_of_new(q, there, i0 + n * kStep);
         x[n] = load4(a.v.x + t * a.v.stride + (int64_t)kh * D * (a.f32 ? 4 : 2), d, a.f32);
     }
 #pragma unroll

@@ -32,6 +32,18 @@ __host__ __device__ inline Seq seq_from(int t0, int t1, int len, int n_tokens, i
     q.pos0 = q.len - q.n;
     return q;
 }
+// Tile `tile` of kTurn positions (base on) of those that are new: [begin, q.len).  V is turned a tile at a time; none: there is nothing new in it.
+constexpr int kTurn = 64;
+struct NewTile { int begin, base; bool none; };
+__host__ __device__ inline NewTile new_tile(const Seq& q, int tile) {
+    NewTile n;
+    n.begin = q.pos0 > 0 ? q.pos0 : 0;
+    n.base = (n.begin & ~(kTurn - 1)) + tile * kTurn;
+    n.none = q.bad || n.begin >= q.len || n.base >= q.len;       // (a sequence without new tokens begins at its end, also inside a tile)
+    return n;
+}
+// The row of the call that position base + i of such a tile is read from: its token's, or another new one's if it is not new itself.
+__host__ __device__ inline int row_of_new(const Seq& q, const NewTile& n, int i) { return q.first + (within(n.base + i, n.begin, q.len - 1) - q.pos0); }
 __host__ __device__ inline int page_or_none(int id, int n_pages) { return id >= 0 && id < n_pages ? id : -1; }
 
 __device__ __forceinline__ Seq seq_at(const SeqArgs& a, int s) {
