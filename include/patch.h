@@ -479,7 +479,8 @@ typedef struct {
 
 /* A batch: sequence s has the tokens q_start[s] .. q_start[s + 1] - 1 of the call's rows, the last of its kv_len[s] tokens in
  * the cache.  So the i-th of its n has position kv_len[s] - n + i.  Sequences of no tokens, or with nothing in the cache, are
- * fine.  A token whose position is negative has no place: it is not appended, and attends to nothing.
+ * fine, and so are rows in front of q_start[0] and from q_start[n_seqs] on, which no sequence has.  A token whose position is
+ * negative has no place: it is not appended, and attends to nothing.
  * The numbers on the device are not read by the host.  Page numbers outside 0 .. n_pages - 1, and lengths beyond max_kv or
  * the table, are not followed: patch_kv_append writes nothing there, and the rows of patch_attention that need them are NaN. */
 typedef struct {
@@ -502,7 +503,8 @@ patch_status patch_qk_rope(const patch_heads* q, const patch_heads* k, const int
 
 /* The new tokens of a batch into the cache: K (normed and rotated by its position if asked for) and V (as it is; v->gamma must
  * be NULL), k->out and v->out unused.  With q (or NULL) also Q, normed and rotated, to q->out for patch_attention, in the same
- * launch.  rope: NULL = no rotation (and eps = 1e-6).  Where two tokens of a batch have the same cell, either's value is in it.
+ * launch (rows without a place become zeros there).  rope: NULL = no rotation (and eps = 1e-6).  Where two tokens of a batch have
+ * the same cell, either's value is in it.
  * Errors as patch_qk_rope. */
 patch_status patch_kv_append(const patch_heads* k, const patch_heads* v, const patch_heads* q, const patch_seqs* seqs, const patch_rope* rope,
                              const patch_kv_cache* cache, void* stream);

@@ -100,7 +100,8 @@ __device__ __forceinline__ int row_limit(const AttnArgs& a, const Span& p, int r
     const int t = p.t0 + r / a.group;
     if (!p.front) return p.pos0 + r / a.group + 1;
     const Seq q = seq_at(a.seqs, seq_of(a.seqs, t));
-    return t - q.first < q.n ? min(a.prefix, q.pos0 + t - q.first + 1) : 0;
+    const int i = place_of(q, t);
+    return i >= 0 ? min(a.prefix, q.pos0 + i + 1) : 0;
 }
 
 // Bits of eight keys' cells from `key` on: ones for those that are in [lo, hi).
@@ -1040,7 +1041,8 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const AttnArgs a) {
     const int t = blockIdx.x, head = blockIdx.y;
     const int seq = seq_of(a.seqs, t);
     const Seq q = seq_at(a.seqs, seq);
-    if (t - q.first >= q.n || t - q.first >= a.seqs.max_q) return;     // no sequence has this token, or it is one too many
+    const int place = place_of(q, t);
+    if (place < 0 || place >= a.seqs.max_q) return;     // no sequence has this token, or it is one too many
     const int own = !a.line_waves ? own_parts(a, q.len) : q.len <= a.prefix ? 0 : as_global(a.unit_parts)[seq * a.cache.kv_heads + head / a.group];
     if (a.prefix_parts == 0 && (own == 1 || (own == 0 && !a.line_waves))) return;     // written by the workgroup itself
     const int parts = a.prefix_parts + own;

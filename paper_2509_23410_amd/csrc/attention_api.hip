@@ -199,6 +199,8 @@ void patch_test_seq(int t0, int t1, int len, int n_tokens, int max_kv, int* out)
     out[0] = q.first; out[1] = q.n; out[2] = q.len; out[3] = q.pos0; out[4] = q.bad;
 }
 int patch_test_page(int id, int n_pages) { return page_or_none(id, n_pages); }
+// ... which of its sequence's tokens a row of the call is, -1: none
+int patch_test_place(int t0, int t1, int n_tokens, int t) { return place_of(seq_from(t0, t1, 1, n_tokens, 1), t); }
 // ... a tile of new positions: whether there are any in it, its bounds, and the row that each of its positions is read from
 void patch_test_new_tile(int t0, int t1, int len, int n_tokens, int max_kv, int tile, int* out) {
     const Seq q = seq_from(t0, t1, len, n_tokens, max_kv);

@@ -126,8 +126,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
     } else {
         const int s = seq_of(a.seqs, (int)t);
         const Seq q = seq_at(a.seqs, s);
-        const int i = (int)t - q.first;
-        pos = !q.bad && i < q.n ? q.pos0 + i : -1;
+        const int i = place_of(q, (int)t);
+        pos = !q.bad && i >= 0 ? q.pos0 + i : -1;
         if (pos >= 0) page = page_or_none(as_global(a.seqs.table)[s * a.seqs.table_stride + (pos >> a.cache.page_log2)], a.cache.n_pages);
     }
     const bool placed = pos >= 0;

@@ -32,6 +32,8 @@ __host__ __device__ inline Seq seq_from(int t0, int t1, int len, int n_tokens, i
     q.pos0 = q.len - q.n;
     return q;
 }
+// Which of its sequence's tokens row t of the call is; -1: rows in front of the first sequence's, or behind the last one's, are nobody's.
+__host__ __device__ inline int place_of(const Seq& q, int t) { return t >= q.first && t - q.first < q.n ? t - q.first : -1; }
 // Tile `tile` of kTurn positions (base on) of those that are new: [begin, q.len).  V is turned a tile at a time; none: there is nothing new in it.
 constexpr int kTurn = 64;
 struct NewTile { int begin, base; bool none; };
@@ -52,7 +54,7 @@ __device__ __forceinline__ Seq seq_at(const SeqArgs& a, int s) {
     return seq_from(as_global(a.q_start)[s], as_global(a.q_start)[s + 1], len, a.n_tokens, a.max_kv);
 }
 
-// The sequence of token t: the last one whose tokens begin at or before t (those without tokens in between are passed over).
+// The sequence of token t, if any has it (place_of tells): the last one whose tokens begin at or before t (those without tokens in between are passed over).
 __device__ __forceinline__ int seq_of(const SeqArgs& a, int t) {
     if (!a.q_start) return min(t, a.n_seqs - 1);
     int lo = 0, hi = a.n_seqs - 1;

@@ -32,3 +32,11 @@ def test_tiles_of_v_read_rows_of_their_sequence_alone(n_tokens, max_kv):
                                 seen.add(base + i)
                 if length <= 3 * TURN:
                     assert seen == (set(range(begin, length)) if n and 0 < length <= max_kv else set())
+
+
+def test_rows_that_no_sequence_has():
+    place = B.lib().patch_test_place
+    for n_tokens in (10, 1 << 23):
+        for t0, t1 in [(0, 3), (3, 5), (3, 3), (10, 10), (4, 10), (0, 10)]:
+            for t in range(10):
+                assert place(t0, t1, n_tokens, t) == (t - t0 if t0 <= t < t1 else -1), (t0, t1, t)
