@@ -92,8 +92,6 @@ static patch_status fill_seqs(SeqArgs* to, const patch_seqs* s, int page_size) {
     int64_t most = s->table_stride * page_size;                       // tokens that a row of the table has pages for
     if (most > (1 << 30)) most = 1 << 30;
     to->max_kv = (int)(s->max_kv < most ? s->max_kv : most);
-    // one token each, and as many tokens as sequences: token s is sequence s's, and nobody need look
-    if (s->max_q == 1 && s->n_tokens == s->n_seqs) to->q_start = nullptr;
     return PATCH_OK;
 }
 

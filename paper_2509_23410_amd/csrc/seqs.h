@@ -56,7 +56,10 @@ __device__ __forceinline__ Seq seq_at(const SeqArgs& a, int s) {
 
 // The sequence of token t, if any has it (place_of tells): the last one whose tokens begin at or before t (those without tokens in between are passed over).
 __device__ __forceinline__ int seq_of(const SeqArgs& a, int t) {
-    if (!a.q_start) return min(t, a.n_seqs - 1);
+    const int same = min(t, a.n_seqs - 1);
+    if (!a.q_start) return same;
+    // where all have one token, sequence t has token t: known after one look
+    if (as_global(a.q_start)[same] <= t && t < as_global(a.q_start)[same + 1]) return same;
     int lo = 0, hi = a.n_seqs - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
