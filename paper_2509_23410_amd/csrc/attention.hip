@@ -1103,7 +1103,8 @@ static int64_t chunk_of(int64_t keys, int64_t units, int block, int64_t grid_uni
 size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     const int D = a->cache.head_dim, heads = a->cache.kv_heads;
     const int64_t rows = (int64_t)a->seqs.n_tokens * a->heads, notes = (int64_t)a->seqs.n_seqs * heads;
-    const int64_t per_part = rows * (D + 2) * 4, room = (int64_t)std::min<size_t>(ws_bytes, (size_t)1 << 60) - 4 * up_to(notes, 4) - 16;
+    const int64_t gap = rows % 2 ? 8 : 0;                     // after the maxima and sums, so that what follows is aligned
+    const int64_t per_part = rows * (D + 2) * 4, room = (int64_t)std::min<size_t>(ws_bytes, (size_t)1 << 60) - 4 * up_to(notes, 4) - gap;
     const int64_t most = room > 0 ? room / per_part : 0;      // parts that the workspace holds
     const auto blocks = [&](int64_t tokens, int block) { return over(tokens * a->group, block); };
     const auto halves = [&](int block) { return D == 256 && block >= 128 ? 2 : 1; };      // workgroups of such a block
@@ -1115,7 +1116,7 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     // Every sequence reads the shared keys as its own where it has to, and where blocks of 128 rows and more, for which reading keys is little of the work, fill
     // the chip without being cut: 32 pieces of 64 tokens, 8 key heads of 4 query heads, behind 2048 shared keys 100 us so, 211 in parts; 6 pieces of 200
     // tokens (192 workgroups) 130 and 109, 8 of 70 behind 8192 (128) 176 and 133.
-    if (most < 3 || a->seqs.n_seqs < 2 || (!a->few && units * a->seqs.n_seqs >= 256)) a->prefix = 0;
+    if (most < (a->few ? 3 : 2) || a->seqs.n_seqs < 2 || (!a->few && units * a->seqs.n_seqs >= 256)) a->prefix = 0;
     const bool line = a->few && (over(a->seqs.max_kv, 32) + 1) * notes < (int64_t)1 << 29;    // its steps are counted in 32 bits
     if (a->few && !line) a->prefix = 0;
     const int64_t own = a->seqs.max_kv - (a->prefix & ~63);
@@ -1148,14 +1149,16 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
         }
         a->own_chunk = (int)up_to(std::max<int64_t>(own, 1), 128);
     } else {
+        int64_t chunk = chunk_of(own, units * a->seqs.n_seqs, block, units);
         if (a->prefix) {
-            int64_t chunk = chunk_of(a->prefix, front_units, front, front_units);
-            if (over(a->prefix, chunk) > most / 2) chunk = up_to(over(a->prefix, most / 2), 128);
-            a->prefix_chunk = (int)chunk;
-            a->prefix_parts = (int)over(a->prefix, chunk);
+            // what the sequences' own keys leave of the workspace, or half of it
+            const int64_t share = std::max(most / 2, most - std::max<int64_t>(over(own, chunk), 1));
+            int64_t shared_chunk = chunk_of(a->prefix, front_units, front, front_units);
+            if (over(a->prefix, shared_chunk) > share) shared_chunk = up_to(over(a->prefix, share), 128);
+            a->prefix_chunk = (int)shared_chunk;
+            a->prefix_parts = (int)over(a->prefix, shared_chunk);
         }
         const int64_t left = most - a->prefix_parts;
-        int64_t chunk = chunk_of(own, units * a->seqs.n_seqs, block, units);
         if (left < 2 && !a->prefix) chunk = up_to(std::max<int64_t>(own, 1), 128);
         else if (over(own, chunk) > left) chunk = up_to(over(own, left), 128);
         a->own_chunk = (int)chunk;
@@ -1166,7 +1169,7 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
     float* at = a->part_ml + 2 * up_to(a->parts * rows, 2);
     a->part_o = at;
     a->unit_parts = reinterpret_cast<int*>(at + (int64_t)a->parts * rows * D);
-    return (size_t)(2 * up_to(a->parts * rows, 2) + (int64_t)a->parts * rows * D + up_to(notes, 4)) * 4;
+    return (size_t)(a->parts * per_part + gap + 4 * up_to(notes, 4));
 }
 
 template <int D, int RB, bool E4M3>
