@@ -511,10 +511,10 @@ patch_status patch_kv_append(const patch_heads* k, const patch_heads* v, const p
 
 typedef struct {
     float scale;             /* of q . k; 0: 1 / sqrt(head_dim)                                                                  */
-    int64_t prefix_len;      /* the first so many tokens of every sequence of the batch are the same ones (of a shorter one, all  */
-                             /* of its tokens are): they are read once for all rows, from the pages of the first sequence that is */
-                             /* that long.  Any number, also inside a page (each sequence then has its own copy of that page for */
-                             /* what follows); 0: nothing shared                                                                 */
+    int64_t prefix_len;      /* the first so many tokens of every sequence of the batch are the same ones (of a shorter one, all */
+                             /* of its tokens are): they are read once for all rows, from the pages of the first sequence with   */
+                             /* tokens in the call that is that long, or of the longest if none is.  Any number, also inside a   */
+                             /* page (each sequence then has its own copy of that page for what follows); 0: nothing shared      */
     float* lse;              /* DEVICE out, n_tokens x heads: the logarithm of the sum of exp(score) over a row's keys; or NULL  */
     void* workspace;         /* DEVICE, 16-byte aligned scratch of the call, or NULL: then nothing is computed once for all and  */
     size_t workspace_bytes;  /* a sequence's keys are not split over workgroups, which is slower for few rows                    */

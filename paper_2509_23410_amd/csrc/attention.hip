@@ -53,22 +53,33 @@ __device__ __forceinline__ Span front_span(const AttnArgs& a, int part) {
     p.rows = a.seqs.n_tokens * a.group;
     p.pos0 = 0;
     p.key0 = 0;
-    p.key1 = a.prefix;
     p.begin = part * a.prefix_chunk;
     p.end = min(a.prefix, p.begin + a.prefix_chunk);
     p.part = part;
     p.bad = false;
-    // the pages are those in the row of the first sequence that has them all: one of padding may be in front of it
-    int s = 0;
+    // The pages are those in the row of the first sequence that has all of the front, or of the longest where none has (no row sees more than that one has).
+    // Only sequences with tokens in the call count: one that is idle may not have its pages any more.
+    int s = 0, longest = 0;
     const int lane = threadIdx.x & 63;
     for (int s0 = 0; s0 < a.seqs.n_seqs; s0 += 64) {
-        const int len = as_global(a.seqs.kv_len)[min(s0 + lane, a.seqs.n_seqs - 1)];
-        const uint64_t there = __ballot(s0 + lane < a.seqs.n_seqs && len >= a.prefix && len <= a.seqs.max_kv);
+        const Seq q = seq_at(a.seqs, min(s0 + lane, a.seqs.n_seqs - 1));
+        const int len = s0 + lane < a.seqs.n_seqs && q.n > 0 && !q.bad ? min(q.len, a.prefix) : 0;
+        const uint64_t there = __ballot(len == a.prefix);
         if (there) {
+            longest = a.prefix;
             s = s0 + __builtin_ctzll(there);
             break;
         }
+        int top = len;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) top = max(top, __shfl_xor(top, m));
+        top = __builtin_amdgcn_readfirstlane(top);
+        if (top > longest) {
+            longest = top;
+            s = s0 + __builtin_ctzll(__ballot(len == top));
+        }
     }
+    p.key1 = longest;
     p.table = __builtin_amdgcn_readfirstlane(s) * a.seqs.table_stride;
     return p;
 }
