@@ -59,7 +59,7 @@ __device__ __forceinline__ int seq_of(const SeqArgs& a, int t) {
     const int same = min(t, a.n_seqs - 1);
     if (!a.q_start) return same;
     // where all have one token, sequence t has token t: known after one look
-    if (as_global(a.q_start)[same] <= t && t < as_global(a.q_start)[same + 1]) return same;
+    if (a.n_tokens == a.n_seqs && as_global(a.q_start)[same] <= t && t < as_global(a.q_start)[same + 1]) return same;
     int lo = 0, hi = a.n_seqs - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
