@@ -482,7 +482,8 @@ typedef struct {
  * fine, and so are rows in front of q_start[0] and from q_start[n_seqs] on, which no sequence has.  A token whose position is
  * negative has no place: it is not appended, and attends to nothing.
  * The numbers on the device are not read by the host.  Page numbers outside 0 .. n_pages - 1, and lengths beyond max_kv or
- * the table, are not followed: patch_kv_append writes nothing there, and the rows of patch_attention that need them are NaN. */
+ * the table, are not followed: patch_kv_append writes nothing there, and the rows of patch_attention that need such a page,
+ * or are of such a sequence, are NaN. */
 typedef struct {
     int64_t n_seqs;             /* 1 .. 65535; times kv_heads at most 2^22 in patch_attention                                    */
     int64_t n_tokens;           /* rows of the call: up to 2^23, and up to 2^25 heads of them in patch_attention                 */

@@ -46,6 +46,9 @@ struct Span {
     bool front, bad;
 };
 
+// What a row's sum is taken for where the result is written: a NaN in a sequence whose length cannot be, also where the row sees nothing of what is there.
+__device__ __forceinline__ float sum_of_row(bool bad, float l) { return bad ? __builtin_nanf("") : l; }
+
 __device__ __forceinline__ Span front_span(const AttnArgs& a, int part) {
     Span p;
     p.front = true;
@@ -181,6 +184,7 @@ __device__ __forceinline__ void attend_row_alone(const AttnArgs& a, const Span& 
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] *= move;
     }
+    l = sum_of_row(p.bad, l);
     const int64_t row = token * a.heads + head, part = (int64_t)p.part * a.seqs.n_tokens * a.heads + row;
     if (lane * E < first || lane * E >= first + features) return;
     const float over = (p.part < 0 ? (l == 0.f ? 0.f : 1.f / l) : 1.f) * v_scale;
@@ -502,6 +506,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, in
             for (int w = 0; w < 4; ++w) mc = fmaxf(mc, sh.m[w][16 * b + c]);
 #pragma unroll
             for (int w = 0; w < 4; ++w) lc += sh.l[w][16 * b + c] * exp2_off(sh.m[w][16 * b + c], mc);
+            lc = sum_of_row(p.bad, lc);
             const int64_t row = (int64_t)(p.t0 + r / a.group) * a.heads + kh * a.group + r % a.group;
             // p.part < 0: the result itself, over its sum (0 where the row sees nothing)
             const float over = (p.part < 0 ? (lc == 0.f ? 0.f : 1.f / lc) : 1.f) * v_scale;
@@ -771,7 +776,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
         for (int i = wave; i < min(32 * NW, p.rows - first_row); i += NW) attend_row_alone<D, E4M3>(a, p, kh, first_row + i, lane, &sh.m[i], half * DV, DV);
         return;
     }
-    l += __shfl_xor(l, 32);
+    l = sum_of_row(p.bad, l + __shfl_xor(l, 32));
     if (!there) return;
     float v_scale = 1.f;
     if (E4M3 && a.cache.v_scale) v_scale = as_global(a.cache.v_scale)[kh];
@@ -992,6 +997,7 @@ __device__ __forceinline__ void attend_line(const AttnArgs& a, int me) {
                     float l = st.l[b];
                     l += __shfl_xor(l, 16);
                     l += __shfl_xor(l, 32);
+                    l = sum_of_row(p.bad, l);
                     if (16 * b + col >= p.rows) continue;
                     const int64_t token = p.t0 + token_of[b];
                     const int head = c.kh * a.group + head_of[b];
@@ -1083,7 +1089,8 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const AttnArgs a) {
         acc += sh_acc[i][lane];
         sum += sh_sum[i];
     }
-    acc *= q.bad ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum;
+    sum = sum_of_row(q.bad, sum);
+    acc *= sum == 0.f ? 0.f : 1.f / sum;
     *reinterpret_cast<PATCH_EP_GLOBAL u32x2_t*>(as_global_out(a.O) + t * a.o_stride + (int64_t)head * D + 4 * lane) =
         u32x2_t{bf16_pair(acc[0], acc[1]), bf16_pair(acc[2], acc[3])};
     if (a.lse && lane == 0) as_global_out(a.lse)[row] = 0.6931471805599453f * (top + __builtin_log2f(sum));
