@@ -446,6 +446,7 @@ typedef struct {
     const float* gamma;  /* DEVICE, head_dim factors, 16-byte aligned: each head becomes x / sqrt(mean(x^2) + eps) * gamma (before */
                          /* the rotation); NULL: no norm                                                                         */
     void* out;           /* DEVICE, bf16, 16-byte aligned, where the call writes such rows; may be x itself where that is bf16   */
+                         /* and the strides are the same, and else may not overlap it                                            */
     int64_t out_stride;  /* its elements from one token to the next, a multiple of 8                                             */
 } patch_heads;
 

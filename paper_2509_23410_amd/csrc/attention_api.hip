@@ -20,8 +20,8 @@ static patch_status launched() {
     return PATCH_ERR_HIP;
 }
 
-// writes: the call writes h->out
-static patch_status fill_heads(HeadArgs* to, const patch_heads* h, int head_dim, int f32, bool writes) {
+// writes: the call writes h->out, for so many tokens
+static patch_status fill_heads(HeadArgs* to, const patch_heads* h, int head_dim, int f32, bool writes, int64_t n_tokens = 0) {
     if (!h->x || h->heads < 1 || h->heads > 16384 || (h->f32 != 0) != (f32 != 0)) return PATCH_ERR_ARG;
     const int size = f32 ? 4 : 2;
     if (!aligned(h->x) || !aligned(h->gamma)) return PATCH_ERR_ARG;
@@ -30,6 +30,8 @@ static patch_status fill_heads(HeadArgs* to, const patch_heads* h, int head_dim,
     if (writes) {
         if (!h->out || !aligned(h->out)) return PATCH_ERR_ARG;
         if (h->out_stride < width || h->out_stride > ((int64_t)1 << 40) || h->out_stride % 8) return PATCH_ERR_SHAPE;
+        // in place a head goes where it came from, or its workgroup would write what another has yet to read
+        if (h->out == h->x && (f32 || (n_tokens > 1 && h->out_stride != h->stride))) return PATCH_ERR_ARG;
     }
     to->x = static_cast<const uint8_t*>(h->x);
     to->stride = h->stride * size;
@@ -108,8 +110,8 @@ patch_status patch_qk_rope(const patch_heads* q, const patch_heads* k, const int
     if (!q || !positions || !aligned(positions, 4) || n_tokens < 0 || n_tokens > (1 << 23)) return PATCH_ERR_ARG;
     if (!head_dim_ok(head_dim)) return PATCH_ERR_SHAPE;
     RopeArgs a = {};
-    TRY(fill_heads(&a.q, q, head_dim, q->f32, true));
-    if (k) TRY(fill_heads(&a.k, k, head_dim, q->f32, true));
+    TRY(fill_heads(&a.q, q, head_dim, q->f32, true, n_tokens));
+    if (k) TRY(fill_heads(&a.k, k, head_dim, q->f32, true, n_tokens));
     TRY(fill_rope(&a, rope, head_dim));
     a.positions = positions;
     a.n_tokens = n_tokens;
@@ -128,7 +130,7 @@ patch_status patch_kv_append(const patch_heads* k, const patch_heads* v, const p
     if (k->heads != cache->kv_heads || v->heads != cache->kv_heads) return PATCH_ERR_SHAPE;
     TRY(fill_heads(&a.k, k, cache->head_dim, k->f32, false));
     TRY(fill_heads(&a.v, v, cache->head_dim, k->f32, false));
-    if (q) TRY(fill_heads(&a.q, q, cache->head_dim, k->f32, true));
+    if (q) TRY(fill_heads(&a.q, q, cache->head_dim, k->f32, true, seqs->n_tokens));
     TRY(fill_rope(&a, rope, cache->head_dim));
     TRY(fill_seqs(&a.seqs, seqs, cache->page_size));
     a.n_tokens = seqs->n_tokens;
