@@ -431,7 +431,7 @@ struct RowsLds {
     int pages[kTableKeys / 16];
 };
 
-// All rows of a span (16 RB at most), by a workgroup of four wavefronts that take its steps in turn; their results meet in LDS.
+// All rows of a sequence's span (16 RB at most), by a workgroup of four wavefronts that take its steps in turn; their results meet in LDS and are written there.
 template <int D, int RB, bool E4M3>
 __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, int kh, RowsLds<D, RB>& sh) {
     typedef StepKeys<D, RB, E4M3> Keys;
@@ -508,32 +508,17 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, in
             for (int w = 0; w < 4; ++w) lc += sh.l[w][16 * b + c] * exp2_off(sh.m[w][16 * b + c], mc);
             lc = sum_of_row(p.bad, lc);
             const int64_t row = (int64_t)(p.t0 + r / a.group) * a.heads + kh * a.group + r % a.group;
-            // p.part < 0: the result itself, over its sum (0 where the row sees nothing)
-            const float over = (p.part < 0 ? (lc == 0.f ? 0.f : 1.f / lc) : 1.f) * v_scale;
-            f32x4_t out[D / 64];
+            const float over = (lc == 0.f ? 0.f : 1.f / lc) * v_scale;                   // (0 where the row sees nothing)
+            const int64_t at = (int64_t)(p.t0 + r / a.group) * a.o_stride + (int64_t)(kh * a.group + r % a.group) * D + d0;
 #pragma unroll
             for (int i = 0; i < D / 64; ++i) {
-                out[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                f32x4_t out = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int w = 0; w < 4; ++w) out[i] += *reinterpret_cast<const f32x4_t*>(&sh.o[w][c][d0 + 4 * i]);
-                out[i] *= over;
+                for (int w = 0; w < 4; ++w) out += *reinterpret_cast<const f32x4_t*>(&sh.o[w][c][d0 + 4 * i]);
+                out *= over;
+                *reinterpret_cast<PATCH_EP_GLOBAL u32x2_t*>(as_global_out(a.O) + at + 4 * i) = u32x2_t{bf16_pair(out[0], out[1]), bf16_pair(out[2], out[3])};
             }
-            if (p.part < 0) {
-                const int64_t at = (int64_t)(p.t0 + r / a.group) * a.o_stride + (int64_t)(kh * a.group + r % a.group) * D + d0;
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i)
-                    *reinterpret_cast<PATCH_EP_GLOBAL u32x2_t*>(as_global_out(a.O) + at + 4 * i) =
-                        u32x2_t{bf16_pair(out[i][0], out[i][1]), bf16_pair(out[i][2], out[i][3])};
-                if (a.lse && d0 == 0) as_global_out(a.lse)[row] = 0.6931471805599453f * (mc + __builtin_log2f(lc));
-            } else {
-                const int64_t at = ((int64_t)p.part * a.seqs.n_tokens * a.heads + row);
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) *reinterpret_cast<PATCH_EP_GLOBAL f32x4_t*>(as_global_out(a.part_o) + at * D + d0 + 4 * i) = out[i];
-                if (d0 == 0) {
-                    as_global_out(a.part_ml)[2 * at] = mc;
-                    as_global_out(a.part_ml)[2 * at + 1] = lc;
-                }
-            }
+            if (a.lse && d0 == 0) as_global_out(a.lse)[row] = 0.6931471805599453f * (mc + __builtin_log2f(lc));
         }
     }
 }
