@@ -141,7 +141,8 @@ __device__ __forceinline__ float cell_value(const uint8_t* base, int64_t i, bool
 }
 
 // One row by one wavefront, key by key and with no key that the row does not see.  In the products of the kernels below a row has 0 times the values of the
-// keys behind it, which is a NaN where those are not finite: workgroups that come across such values do their rows again here.  Slow, and hardly ever run.
+// keys behind it, which is a NaN where those are not finite: workgroups that come across such values do their rows again here.  Slow, and hardly ever run: a
+// prompt of 1024 over 32 heads of 128 takes 68 us, and 7.5 ms with an infinity in its last key.
 // It writes `features` of the head from `first` on, its sums held against *against (null: against the row's maximum), so that another workgroup's others fit.
 template <int D, bool E4M3>
 __device__ __forceinline__ void attend_row_alone(const AttnArgs& a, const Span& p, int kh, int r, int lane, const float* against, int first, int features) {
@@ -524,8 +525,9 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, in
 }
 
 // Many rows: a workgroup's wavefronts have 32 rows each, and the keys come through LDS for all of them, kTile at a time, the next ones on their way through
-// registers meanwhile.  The products are the ones above on 32 x 32 x 16 instructions.  A prompt of 4096 over 32 heads of 128: 167 - 175 us, 825 - 785 TFLOP/s;
-// with operands from registers alone it would be 116, with the reads from LDS (all of K and V for each wavefront) and no softmax 160: those two bound it.
+// registers meanwhile.  The products are the ones above on 32 x 32 x 16 instructions.  A prompt of 4096 over 32 heads of 128: 167 - 178 us on different cards,
+// 825 - 770 TFLOP/s; with operands from registers alone it would be 116, with the reads from LDS (all of K and V for each wavefront) and no softmax 160: those
+// two bound it.  27 % of the LDS' busy cycles are bank conflicts; which of its reads and writes have them has not been found out.
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 // Where 16-byte chunk c of a row lies in LDS: the same chunk of 8 rows side by side is in 8 different places of 128 bytes, of 16 rows in 16 of 256
@@ -1130,8 +1132,10 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
         const int64_t resident = kResident / 2 * rows_resident(D, block / 16);
         int64_t own_blocks = resident;
         if (a->prefix) {
-            // What both cost in workgroups' time where all share the memory, in us: 64 keys for 128 rows of the front 3, 128 keys of a sequence 7 (heads of 128 in
-            // bf16); the longest sequence is known, and the others are taken to be half as long on the whole.
+            // What both cost in workgroups' time where all share the memory, in us: 64 keys for 128 rows of the front 3, 128 keys of a sequence 7, in e4m3 half of
+            // that.  Taken at heads of 128 in bf16 and used for the other sizes too, as a ratio.  The longest sequence is all that the host knows, and the
+            // others are taken to be half as long on the whole: right within a factor of two or so where max_kv is close to the lengths, and if it is far
+            // beyond them the front has too few workgroups (64 sequences of up to 9000 tokens, 8192 shared, the same inputs each time: 47 us, and 238 with max_kv = 65536).
             const double f = 3.0 * front_units * over(a->prefix, 64), o = (a->cache.e4m3 ? 3.5 : 7.0) * 0.5 * notes * over(std::max<int64_t>(own, 1), 128);
             const int64_t share = (int64_t)(resident * f / (f + o));
             int64_t parts = std::max<int64_t>(over(share, front_units), 1);

@@ -10,7 +10,8 @@
 namespace patch {
 
 // V of a tile of 64 positions of one sequence and key head, turned in LDS: a feature's tokens side by side, as the page holds them.  By itself each value is a
-// store of its own, a page's tokens apart: two prompts of 1100 tokens, 32 key heads of 128, e4m3, 70.3 us, in tiles 37.9.
+// store of its own, a page's tokens apart: two prompts of 1100 tokens, 32 key heads of 128, e4m3, 70.3 us, in tiles 37.9 (and
+// 33.1 with several heads a thread for Q and K).
 template <int D>
 __device__ __forceinline__ void append_v_tile(const RopeArgs& a, int tile, int kh, int s) {
     __shared__ uint16_t sh_v[D][kTurn + 2];                      // bf16, or e4m3 in the low byte; rows an odd number of words apart
