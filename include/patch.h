@@ -537,6 +537,84 @@ patch_status patch_attention(const void* Q, int64_t q_stride, int heads, const p
 /* The scratch with which that call splits its keys as finely as it would like (of opts only prefix_len is looked at); 0 for arguments that it refuses. */
 size_t patch_attention_workspace_bytes(int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const patch_attention_opts* opts);
 
+/* ---- A cache that holds more: cells of 4 bits, and fewer tokens ----------------------------------------------------
+ * As above: asynchronous on `stream`, nothing allocated, no synchronisation, may be captured, the same bits every time. */
+
+/* The cache of one layer in 4 bits.  A cell is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 .. 7; + 8: negative) times a power of two that
+ * features 32 b .. 32 b + 31 of a token share: a byte, 2^(byte - 127), 255 for a NaN.  So 17 bytes hold 32 values.  A page holds, for
+ * every key head in turn, in `k` page_size x head_dim / 2 bytes, token-major, feature 2 j in the low four bits of byte j; in `v`
+ * head_dim / 2 x page_size bytes: pair-major, the tokens of features 2 j (low) and 2 j + 1 side by side; and their powers in k_scale,
+ * page_size x head_dim / 32, and in v_scale, head_dim / 32 x page_size. */
+typedef struct {
+    void* k;                 /* DEVICE, 16-byte aligned                                                                          */
+    void* v;                 /* DEVICE, 16-byte aligned                                                                          */
+    void* k_scale;           /* DEVICE, 16-byte aligned                                                                          */
+    void* v_scale;           /* DEVICE, 16-byte aligned                                                                          */
+    int64_t n_pages;         /* up to 2^31 - 1                                                                                   */
+    int64_t page_stride;     /* cells from one page to the next, in k and in v, a multiple of 512, less than 2^33 (in bytes the half of */
+                             /* that; 1 / 32 in the scales); 0: pages lie side by side                                           */
+    int page_size;           /* tokens: 16, 32, 64, 128 or 256                                                                   */
+    int kv_heads, head_dim;  /* head_dim: 64, 128 or 256                                                                         */
+} patch_kv_cache4;
+
+/* patch_kv_append into 4-bit cells.  The power of 32 values is the smallest of which the largest magnitude is at most seven, from 2^-100 to
+ * 2^125; a cell is the value over the power rounded to the nearest, ties to even codes, and six where it is beyond six.  32 values one
+ * of which is a NaN or infinite become NaN.
+ *   k->out, v->out  bf16 rows for what the new tokens' cells stand for (exact in bf16), or NULL; rows without a place become zeros
+ *   positions       DEVICE, n_tokens: where the rotation takes a token to be, for caches that tokens were evicted from; one outside
+ *                   0 .. n_pos - 1 turns by NaN.  NULL: its position in the cache.
+ * Errors as patch_kv_append. */
+patch_status patch_kv_append4(const patch_heads* k, const patch_heads* v, const patch_heads* q, const patch_seqs* seqs, const patch_rope* rope,
+                              const int32_t* positions, const patch_kv_cache4* cache, void* stream);
+
+/* patch_attention over 4-bit cells. */
+patch_status patch_attention4(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache4* cache, void* O, int64_t o_stride,
+                              void* stream, const patch_attention_opts* opts);
+size_t patch_attention4_workspace_bytes(int heads, const patch_seqs* seqs, const patch_kv_cache4* cache, const patch_attention_opts* opts);
+
+typedef struct {
+    float scale;              /* of q . k; 0: 1 / sqrt(head_dim)                                                                 */
+    float decay;              /* what a weight keeps of itself                                                                   */
+    const int32_t* positions; /* DEVICE, n_tokens, or NULL                                                                       */
+    int32_t* slot_positions;  /* DEVICE, laid out as the weights, or NULL: positions of the call's tokens go to their slots      */
+} patch_weights_opts;
+
+/* How much the cached tokens have been attended to:
+ *   W_out[s][h][j] = decay W[s][h][j] + sum of exp(scale q[t, g] . k[j, h] - lse[t, g])
+ * over the call's tokens t of sequence s that see key j and the query heads g of key head h; keys that the call brought have no weight
+ * before it (W is not read there).  For sequences with tokens in the call and j < kv_len[s]; everything else stays as it is.
+ *   Q, q_stride, heads  as in patch_attention, whose lse (n_tokens x heads) for these rows is `lse`
+ *   W, W_out            DEVICE, n_seqs x kv_heads rows of `stride` >= max_kv floats, 16-byte aligned, stride a multiple of 4; W_out may be W
+ * A row whose lse is minus infinity (it saw nothing) adds nothing.  Sums are fp32, in an order that the sizes alone decide.  Pages that are
+ * not followed have NaN for keys.  Errors: PATCH_ERR_ARG, PATCH_ERR_SHAPE, PATCH_ERR_HIP. */
+patch_status patch_attention_weights(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const float* lse,
+                                     const float* W, float* W_out, int64_t stride, void* stream, const patch_weights_opts* opts);
+patch_status patch_attention_weights4(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache4* cache, const float* lse,
+                                      const float* W, float* W_out, int64_t stride, void* stream, const patch_weights_opts* opts);
+
+typedef struct {
+    int64_t keep;             /* tokens that a sequence may have afterwards, 1 .. 2^29; shorter ones keep all                    */
+    int64_t sinks, recent;    /* of them stay always: those at positions below sinks, and the `recent` last ones (positions above the */
+                              /* largest minus recent); sinks + recent <= keep                                                   */
+    const int32_t* positions; /* DEVICE, laid out as the weights: the position of each slot's token, or NULL: its slot           */
+    int32_t* positions_out;   /* DEVICE, the same, where slots below keep get theirs afterwards, may be `positions`; or NULL     */
+    float* W_out;             /* DEVICE, laid out as the weights, where slots below keep get theirs afterwards; may be W; or NULL */
+    int32_t* from;            /* DEVICE out, n_seqs x kv_heads x keep: the slot that slot i's token was in before, -1: it has none */
+    int32_t* kv_len_out;      /* DEVICE out, n_seqs: tokens afterwards; may be seqs->kv_len                                      */
+} patch_evict_opts;
+
+/* Each key head of each sequence keeps `keep` of its tokens: those that always stay, then those of the largest weight W (a NaN is the
+ * smallest); of equal ones, and of those that always stay if there are more than `keep`, those in lower slots.  Tokens in slots below
+ * `keep` that stay do so where they are; the others, in the order of their slots, move into the slots there that became free, in
+ * theirs.  So keys are in no order afterwards and differ from head to head: new tokens are appended behind them as always, with
+ * positions given for their rotation.
+ *   seqs   n_seqs, kv_len, page_table, table_stride and max_kv; n_tokens, q_start and max_q are not looked at
+ *   W      DEVICE, n_seqs x kv_heads rows of `stride` >= max_kv floats, 16-byte aligned, stride a multiple of 4
+ * Pages that two sequences share may only be in front of their sinks.  Cells whose page, or whose goal's, is not followed stay; a
+ * sequence longer than max_kv or the table stays as it is (`from` is -1).  Errors: PATCH_ERR_ARG, PATCH_ERR_SHAPE, PATCH_ERR_HIP. */
+patch_status patch_kv_evict(const patch_seqs* seqs, const patch_kv_cache* cache, const float* W, int64_t stride, const patch_evict_opts* opts, void* stream);
+patch_status patch_kv_evict4(const patch_seqs* seqs, const patch_kv_cache4* cache, const float* W, int64_t stride, const patch_evict_opts* opts, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

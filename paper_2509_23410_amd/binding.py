@@ -26,6 +26,7 @@ EXPORTS = [
     "patch_packed_tile_map", "patch_packed_row_order", "patch_probe_matrix_rate", "patch_probe_stream_read", "patch_probe_lds_fill", "patch_probe_store_tiles", "patch_probe_lds_read", "patch_gemm4_ex",
     "patch_serialized_bytes", "patch_serialize", "patch_deserialize", "patch_serialized4_bytes", "patch_serialize4", "patch_deserialize4", "patch_free", "patch_strerror", "patch_last_hip_error", "patch_version",
     "patch_qk_rope", "patch_kv_append", "patch_attention", "patch_attention_workspace_bytes",
+    "patch_kv_append4", "patch_attention4", "patch_attention4_workspace_bytes", "patch_attention_weights", "patch_attention_weights4", "patch_kv_evict", "patch_kv_evict4",
 ]
 
 
@@ -58,9 +59,23 @@ class _KVCacheC(ctypes.Structure):
                 ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("e4m3", ctypes.c_int), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
+class _KVCache4C(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("page_size", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
 class _SeqsC(ctypes.Structure):
     _fields_ = [("n_seqs", ctypes.c_int64), ("n_tokens", ctypes.c_int64), ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
                 ("table_stride", ctypes.c_int64), ("max_q", ctypes.c_int64), ("max_kv", ctypes.c_int64)]
+
+
+class WeightsOpts(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("decay", ctypes.c_float), ("positions", ctypes.c_void_p), ("slot_positions", ctypes.c_void_p)]
+
+
+class EvictOpts(ctypes.Structure):
+    _fields_ = [("keep", ctypes.c_int64), ("sinks", ctypes.c_int64), ("recent", ctypes.c_int64), ("positions", ctypes.c_void_p),
+                ("positions_out", ctypes.c_void_p), ("W_out", ctypes.c_void_p), ("from", ctypes.c_void_p), ("kv_len_out", ctypes.c_void_p)]
 
 
 class AttentionOpts(ctypes.Structure):
@@ -170,6 +185,17 @@ def lib() -> ctypes.CDLL:
         L.patch_last_hip_error.restype = ci
         L.patch_version.restype = ctypes.c_char_p
         pH, pR, pC, pS, pA = (ctypes.POINTER(t) for t in (_HeadsC, _RopeC, _KVCacheC, _SeqsC, AttentionOpts))
+        pC4, pW, pE = (ctypes.POINTER(t) for t in (_KVCache4C, WeightsOpts, EvictOpts))
+        L.patch_kv_append4.argtypes = [pH, pH, pH, pS, pR, vp, pC4, vp]
+        L.patch_attention4.argtypes = [vp, i64, ci, pS, pC4, vp, i64, vp, pA]
+        L.patch_attention4_workspace_bytes.argtypes = [ci, pS, pC4, pA]
+        L.patch_attention4_workspace_bytes.restype = sz
+        for sfx, cache in (("", pC), ("4", pC4)):
+            getattr(L, f"patch_attention_weights{sfx}").argtypes = [vp, i64, ci, pS, cache, vp, vp, vp, i64, vp, pW]
+            getattr(L, f"patch_attention_weights{sfx}").restype = ci
+            getattr(L, f"patch_kv_evict{sfx}").argtypes = [pS, cache, vp, i64, pE, vp]
+            getattr(L, f"patch_kv_evict{sfx}").restype = ci
+        L.patch_kv_append4.restype = L.patch_attention4.restype = ci
         L.patch_qk_rope.argtypes = [pH, pH, vp, i64, ci, pR, vp]
         L.patch_kv_append.argtypes = [pH, pH, pH, pS, pR, pC, vp]
         L.patch_attention.argtypes = [vp, i64, ci, pS, pC, vp, i64, vp, pA]
@@ -611,6 +637,14 @@ class KVCache(_Described):
                          k, v, k_scale, v_scale)
 
 
+class KVCache4(_Described):
+    """The paged keys and values of one layer in 4 bits: k is n_pages x kv_heads x page_size x head_dim / 2 bytes, v is n_pages x kv_heads x
+    head_dim / 2 x page_size, the bytes of their powers of two k_scale and v_scale the same with head_dim / 32; see patch_kv_cache4 in patch.h."""
+
+    def __init__(self, k, v, k_scale, v_scale, n_pages: int, page_size: int, kv_heads: int, head_dim: int, page_stride: int = 0):
+        super().__init__(_KVCache4C(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages, page_stride, page_size, kv_heads, head_dim), k, v, k_scale, v_scale)
+
+
 class Seqs(_Described):
     """A batch of sequences (device int32 kv_len, page_table and q_start); see patch_seqs in patch.h."""
 
@@ -628,18 +662,76 @@ def patch_kv_append(k: Heads, v: Heads, seqs: Seqs, cache: KVCache, stream: int 
     _check(lib().patch_kv_append(k.ref, v.ref, q.ref if q else None, seqs.ref, rope.ref if rope else None, cache.ref, stream), "patch_kv_append")
 
 
-def patch_attention(Q, heads: int, seqs: Seqs, cache: KVCache, O, stream: int = 0, scale: float = 0.0, prefix_len: int = 0, lse=None, workspace=None,
-                    workspace_bytes=None, q_stride: int = 0, o_stride: int = 0) -> None:
-    """O = causal attention of the batch's rows of Q over its pages, the first prefix_len tokens of every sequence read once for all.  Strides in
-    elements (0: rows side by side).  workspace: a device tensor (or pointer + workspace_bytes) of the call's own; see patch.h."""
+def _attention(call, name, Q, heads, seqs, cache, O, stream, scale, prefix_len, lse, workspace, workspace_bytes, q_stride, o_stride) -> None:
     if workspace is not None and workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size()
     width = heads * cache.c.head_dim
     o = AttentionOpts(scale, prefix_len, _ptr(lse), _ptr(workspace), workspace_bytes or 0)
-    _check(lib().patch_attention(_ptr(Q), q_stride or width, heads, seqs.ref, cache.ref, _ptr(O), o_stride or width, stream, ctypes.byref(o)),
-           "patch_attention")
+    _check(call(_ptr(Q), q_stride or width, heads, seqs.ref, cache.ref, _ptr(O), o_stride or width, stream, ctypes.byref(o)), name)
+
+
+def patch_attention(Q, heads: int, seqs: Seqs, cache: KVCache, O, stream: int = 0, scale: float = 0.0, prefix_len: int = 0, lse=None, workspace=None,
+                    workspace_bytes=None, q_stride: int = 0, o_stride: int = 0) -> None:
+    """O = causal attention of the batch's rows of Q over its pages, the first prefix_len tokens of every sequence read once for all.  Strides in
+    elements (0: rows side by side).  workspace: a device tensor (or pointer + workspace_bytes) of the call's own; see patch.h."""
+    _attention(lib().patch_attention, "patch_attention", Q, heads, seqs, cache, O, stream, scale, prefix_len, lse, workspace, workspace_bytes, q_stride, o_stride)
 
 
 def patch_attention_workspace_bytes(heads: int, seqs: Seqs, cache: KVCache, prefix_len: int = 0) -> int:
     o = AttentionOpts(0.0, prefix_len, None, None, 0)
     return int(lib().patch_attention_workspace_bytes(heads, seqs.ref, cache.ref, ctypes.byref(o)))
+
+
+def patch_kv_append4(k: Heads, v: Heads, seqs: Seqs, cache: KVCache4, stream: int = 0, rope=None, q=None, positions=None) -> None:
+    """patch_kv_append into 4-bit cells.  k.out, v.out: what the cells stand for, where given; positions: where the rotation takes the tokens to be
+    (device int32, n_tokens), where that is not their place in the cache."""
+    _check(lib().patch_kv_append4(k.ref, v.ref, q.ref if q else None, seqs.ref, rope.ref if rope else None, _ptr(positions), cache.ref, stream), "patch_kv_append4")
+
+
+def patch_attention4(Q, heads: int, seqs: Seqs, cache: KVCache4, O, stream: int = 0, scale: float = 0.0, prefix_len: int = 0, lse=None, workspace=None,
+                     workspace_bytes=None, q_stride: int = 0, o_stride: int = 0) -> None:
+    """patch_attention over 4-bit cells."""
+    _attention(lib().patch_attention4, "patch_attention4", Q, heads, seqs, cache, O, stream, scale, prefix_len, lse, workspace, workspace_bytes, q_stride, o_stride)
+
+
+def patch_attention4_workspace_bytes(heads: int, seqs: Seqs, cache: KVCache4, prefix_len: int = 0) -> int:
+    o = AttentionOpts(0.0, prefix_len, None, None, 0)
+    return int(lib().patch_attention4_workspace_bytes(heads, seqs.ref, cache.ref, ctypes.byref(o)))
+
+
+def _weights(call, name, Q, heads, seqs, cache, lse, W, W_out, stride, stream, decay, scale, positions, slot_positions, q_stride) -> None:
+    o = WeightsOpts(scale, decay, _ptr(positions), _ptr(slot_positions))
+    _check(call(_ptr(Q), q_stride or heads * cache.c.head_dim, heads, seqs.ref, cache.ref, _ptr(lse), _ptr(W), _ptr(W_out), stride, stream, ctypes.byref(o)), name)
+
+
+def patch_attention_weights(Q, heads: int, seqs: Seqs, cache: KVCache, lse, W, W_out, stride: int, stream: int = 0, decay: float = 1.0, scale: float = 0.0,
+                            positions=None, slot_positions=None, q_stride: int = 0) -> None:
+    """W_out = decay W + every cached token's sum of the attention weights that the batch's rows gave it (lse: patch_attention's of the same rows); W and
+    W_out are n_seqs x kv_heads rows of `stride` floats and may be the same.  slot_positions: laid out so, gets the `positions` of the batch's tokens."""
+    _weights(lib().patch_attention_weights, "patch_attention_weights", Q, heads, seqs, cache, lse, W, W_out, stride, stream, decay, scale, positions, slot_positions, q_stride)
+
+
+def patch_attention_weights4(Q, heads: int, seqs: Seqs, cache: KVCache4, lse, W, W_out, stride: int, stream: int = 0, decay: float = 1.0, scale: float = 0.0,
+                             positions=None, slot_positions=None, q_stride: int = 0) -> None:
+    """patch_attention_weights over 4-bit cells."""
+    _weights(lib().patch_attention_weights4, "patch_attention_weights4", Q, heads, seqs, cache, lse, W, W_out, stride, stream, decay, scale, positions, slot_positions,
+             q_stride)
+
+
+def _evict(call, name, seqs, cache, W, W_out, stride, keep, moved_from, kv_len_out, stream, sinks, recent, positions, positions_out) -> None:
+    o = EvictOpts(keep, sinks, recent, _ptr(positions), _ptr(positions_out), _ptr(W_out), _ptr(moved_from), _ptr(kv_len_out))
+    _check(call(seqs.ref, cache.ref, _ptr(W), stride, ctypes.byref(o), stream), name)
+
+
+def patch_kv_evict(seqs: Seqs, cache: KVCache, W, W_out, stride: int, keep: int, moved_from, kv_len_out, stream: int = 0, sinks: int = 0, recent: int = 0,
+                   positions=None, positions_out=None) -> None:
+    """Each key head of each sequence keeps `keep` tokens: the first `sinks`, the last `recent`, and those of the largest weight W (n_seqs x kv_heads rows of
+    `stride` floats).  Those behind slot `keep` move into the slots that became free; W_out and positions_out (may be W and positions, or None) follow.
+    moved_from (device int32, n_seqs x kv_heads x keep): the slot that each slot's token came from; kv_len_out: tokens afterwards."""
+    _evict(lib().patch_kv_evict, "patch_kv_evict", seqs, cache, W, W_out, stride, keep, moved_from, kv_len_out, stream, sinks, recent, positions, positions_out)
+
+
+def patch_kv_evict4(seqs: Seqs, cache: KVCache4, W, W_out, stride: int, keep: int, moved_from, kv_len_out, stream: int = 0, sinks: int = 0, recent: int = 0,
+                    positions=None, positions_out=None) -> None:
+    """patch_kv_evict of 4-bit cells."""
+    _evict(lib().patch_kv_evict4, "patch_kv_evict4", seqs, cache, W, W_out, stride, keep, moved_from, kv_len_out, stream, sinks, recent, positions, positions_out)

@@ -16,11 +16,15 @@ struct SeqArgs {
     int max_kv;               // no more than table_stride pages hold
 };
 
+enum Cells : int { kBf16 = 0, kE4m3 = 1, kE2m1 = 2 };
+
 struct CacheArgs {
-    uint8_t *k, *v;           // pages: kv_heads x page x head_dim and kv_heads x head_dim x page cells
+    uint8_t *k, *v;           // pages: kv_heads x page x head_dim and kv_heads x head_dim x page cells (e2m1: kv_heads x head_dim / 2 x page pairs of V's features)
     int64_t page_bytes;       // from one page to the next
     const float *k_scale, *v_scale;   // per head, or null: 1
-    int n_pages, page_log2, kv_heads, head_dim, e4m3;
+    uint8_t *k_power, *v_power;       // e2m1: kv_heads x page x head_dim / 32 and kv_heads x head_dim / 32 x page powers of two
+    int64_t power_bytes;              // from one page's to the next
+    int n_pages, page_log2, kv_heads, head_dim, cells;
 };
 
 struct HeadArgs {
@@ -44,6 +48,7 @@ struct RopeArgs {
     float eps;
 };
 void launch_rope(const RopeArgs& a, hipStream_t stream);
+void launch_append4(const RopeArgs& a, hipStream_t stream);   // into cells of 4 bits; positions: of the rotation alone
 
 struct AttnArgs {
     const uint16_t* Q;
@@ -68,5 +73,36 @@ struct AttnArgs {
 // fills all that from own_chunk on for a workspace of ws_bytes (0: none), prefix too where it does without; returns the bytes used
 size_t plan_attention(AttnArgs* a, size_t ws_bytes);
 void launch_attention(const AttnArgs& a, hipStream_t stream);
+void launch_attention4(const AttnArgs& a, hipStream_t stream);     // its kernels for cells of 4 bits, without the joining of parts
+
+struct WeighArgs {
+    const uint16_t* Q;
+    const float* lse;         // n_tokens x heads
+    int64_t q_stride;         // elements
+    const float* w;
+    float* w_out;             // n_seqs x kv_heads rows, w_stride apart
+    int64_t w_stride;
+    const int32_t* positions; // of the call's tokens, or null
+    int32_t* slot_positions;
+    SeqArgs seqs;
+    CacheArgs cache;
+    int heads, group;
+    float scale, decay;       // scale times log2(e)
+};
+void launch_weigh(const WeighArgs& a, hipStream_t stream);
+
+struct EvictArgs {
+    const float* w;
+    float* w_out;             // or null
+    int64_t w_stride;
+    const int32_t* positions; // or null: slots
+    int32_t* positions_out;   // or null
+    int32_t* from;            // n_seqs x kv_heads x keep
+    int32_t* kv_len_out;
+    SeqArgs seqs;
+    CacheArgs cache;
+    int keep, sinks, recent;
+};
+void launch_evict(const EvictArgs& a, hipStream_t stream);
 
 }  // namespace patch

@@ -75,7 +75,32 @@ static patch_status fill_cache(CacheArgs* to, const patch_kv_cache* c) {
     to->page_log2 = log2;
     to->kv_heads = c->kv_heads;
     to->head_dim = c->head_dim;
-    to->e4m3 = c->e4m3 != 0;
+    to->cells = c->e4m3 ? kE4m3 : kBf16;
+    return PATCH_OK;
+}
+
+static patch_status fill_cache(CacheArgs* to, const patch_kv_cache4* c) {
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale || !aligned(c->k) || !aligned(c->v) || !aligned(c->k_scale) || !aligned(c->v_scale)) return PATCH_ERR_ARG;
+    if (c->n_pages < 1 || c->n_pages > INT32_MAX || c->kv_heads < 1 || c->kv_heads > 65535) return PATCH_ERR_ARG;
+    if (!head_dim_ok(c->head_dim)) return PATCH_ERR_SHAPE;
+    int log2 = 4;
+    while (log2 < 8 && (1 << log2) != c->page_size) ++log2;
+    if ((1 << log2) != c->page_size) return PATCH_ERR_SHAPE;
+    const int64_t cells = (int64_t)c->kv_heads * c->page_size * c->head_dim;
+    if (c->page_stride != 0 && (c->page_stride < cells || c->page_stride > ((int64_t)1 << 40) || c->page_stride % 512)) return PATCH_ERR_SHAPE;
+    const int64_t stride = c->page_stride ? c->page_stride : cells;   // (a page of one head is 1024 cells at least)
+    if (stride / 2 >= ((int64_t)1 << 32)) return PATCH_ERR_SHAPE;
+    to->k = static_cast<uint8_t*>(c->k);
+    to->v = static_cast<uint8_t*>(c->v);
+    to->page_bytes = stride / 2;
+    to->k_power = static_cast<uint8_t*>(c->k_scale);
+    to->v_power = static_cast<uint8_t*>(c->v_scale);
+    to->power_bytes = stride / 32;
+    to->n_pages = (int)c->n_pages;
+    to->page_log2 = log2;
+    to->kv_heads = c->kv_heads;
+    to->head_dim = c->head_dim;
+    to->cells = kE2m1;
     return PATCH_OK;
 }
 
@@ -141,7 +166,30 @@ patch_status patch_kv_append(const patch_heads* k, const patch_heads* v, const p
     return launched();
 }
 
-static patch_status fill_attention(AttnArgs* a, int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const patch_attention_opts* opts) {
+patch_status patch_kv_append4(const patch_heads* k, const patch_heads* v, const patch_heads* q, const patch_seqs* seqs, const patch_rope* rope,
+                              const int32_t* positions, const patch_kv_cache4* cache, void* stream) {
+    if (!k || !v || !seqs || !cache || v->gamma || !aligned(positions, 4)) return PATCH_ERR_ARG;
+    RopeArgs a = {};
+    TRY(fill_cache(&a.cache, cache));
+    if (k->heads != cache->kv_heads || v->heads != cache->kv_heads) return PATCH_ERR_SHAPE;
+    TRY(fill_heads(&a.k, k, cache->head_dim, k->f32, k->out != nullptr, seqs->n_tokens));
+    TRY(fill_heads(&a.v, v, cache->head_dim, k->f32, v->out != nullptr, seqs->n_tokens));
+    if (q) TRY(fill_heads(&a.q, q, cache->head_dim, k->f32, true, seqs->n_tokens));
+    TRY(fill_rope(&a, rope, cache->head_dim));
+    TRY(fill_seqs(&a.seqs, seqs, cache->page_size));
+    a.positions = positions;
+    a.n_tokens = seqs->n_tokens;
+    a.head_dim = cache->head_dim;
+    a.f32 = k->f32 != 0;
+    if (seqs->n_tokens == 0) return PATCH_OK;
+    launch_append4(a, static_cast<hipStream_t>(stream));
+    return launched();
+}
+
+}  // extern "C"
+
+template <typename Cache>
+static patch_status fill_attention(AttnArgs* a, int heads, const patch_seqs* seqs, const Cache* cache, const patch_attention_opts* opts) {
     if (!seqs || !cache || heads < 1 || heads > 65535) return PATCH_ERR_ARG;
     TRY(fill_cache(&a->cache, cache));
     TRY(fill_seqs(&a->seqs, seqs, cache->page_size));
@@ -156,8 +204,9 @@ static patch_status fill_attention(AttnArgs* a, int heads, const patch_seqs* seq
     return PATCH_OK;
 }
 
-patch_status patch_attention(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache* cache, void* O, int64_t o_stride,
-                             void* stream, const patch_attention_opts* opts) {
+template <typename Cache>
+static patch_status attend(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const Cache* cache, void* O, int64_t o_stride, void* stream,
+                           const patch_attention_opts* opts) {
     if (!Q || !O || !aligned(Q) || !aligned(O)) return PATCH_ERR_ARG;
     AttnArgs a = {};
     TRY(fill_attention(&a, heads, seqs, cache, opts));
@@ -187,10 +236,103 @@ patch_status patch_attention(const void* Q, int64_t q_stride, int heads, const p
     return launched();
 }
 
-size_t patch_attention_workspace_bytes(int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const patch_attention_opts* opts) {
+template <typename Cache>
+static size_t workspace_bytes(int heads, const patch_seqs* seqs, const Cache* cache, const patch_attention_opts* opts) {
     AttnArgs a = {};
     if (fill_attention(&a, heads, seqs, cache, opts) != PATCH_OK || seqs->n_tokens == 0 || seqs->max_q == 0) return 0;
     return plan_attention(&a, (size_t)1 << 62);
+}
+
+template <typename Cache>
+static patch_status weigh(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const Cache* cache, const float* lse, const float* W, float* W_out,
+                          int64_t stride, void* stream, const patch_weights_opts* opts) {
+    if (!Q || !seqs || !cache || !lse || !W || !W_out || !opts || heads < 1 || heads > 65535) return PATCH_ERR_ARG;
+    if (!aligned(Q) || !aligned(lse, 4) || !aligned(W) || !aligned(W_out) || !aligned(opts->positions, 4) || !aligned(opts->slot_positions, 4)) return PATCH_ERR_ARG;
+    if (!(fabsf(opts->scale) <= 3e38f) || !(fabsf(opts->decay) <= 3e38f) || (opts->slot_positions && !opts->positions)) return PATCH_ERR_ARG;
+    WeighArgs a = {};
+    TRY(fill_cache(&a.cache, cache));
+    TRY(fill_seqs(&a.seqs, seqs, cache->page_size));
+    if (heads % cache->kv_heads) return PATCH_ERR_SHAPE;
+    const int64_t width = (int64_t)heads * cache->head_dim;
+    if (q_stride < width || q_stride > ((int64_t)1 << 40) || q_stride % 8) return PATCH_ERR_SHAPE;
+    if (stride < a.seqs.max_kv || stride > ((int64_t)1 << 32) || stride % 4) return PATCH_ERR_SHAPE;
+    if (seqs->n_tokens * heads > (1 << 25) || seqs->n_seqs * cache->kv_heads > (1 << 22)) return PATCH_ERR_SHAPE;
+    a.Q = static_cast<const uint16_t*>(Q);
+    a.lse = lse;
+    a.q_stride = q_stride;
+    a.w = W;
+    a.w_out = W_out;
+    a.w_stride = stride;
+    a.positions = opts->positions;
+    a.slot_positions = opts->slot_positions;
+    a.heads = heads;
+    a.group = heads / cache->kv_heads;
+    a.scale = (opts->scale != 0.f ? opts->scale : 1.f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
+    a.decay = opts->decay;
+    if (seqs->n_tokens == 0 || seqs->max_q == 0 || a.seqs.max_kv == 0) return PATCH_OK;
+    launch_weigh(a, static_cast<hipStream_t>(stream));
+    return launched();
+}
+
+template <typename Cache>
+static patch_status evict(const patch_seqs* seqs, const Cache* cache, const float* W, int64_t stride, const patch_evict_opts* opts, void* stream) {
+    if (!seqs || !cache || !W || !opts || !opts->from || !opts->kv_len_out) return PATCH_ERR_ARG;
+    if (!aligned(W) || !aligned(opts->W_out) || !aligned(opts->positions) || !aligned(opts->positions_out) || !aligned(opts->from, 4) || !aligned(opts->kv_len_out, 4))
+        return PATCH_ERR_ARG;
+    if (opts->keep < 1 || opts->keep > (1 << 29) || opts->sinks < 0 || opts->recent < 0 || opts->sinks > opts->keep || opts->recent > opts->keep - opts->sinks)
+        return PATCH_ERR_ARG;
+    EvictArgs a = {};
+    TRY(fill_cache(&a.cache, cache));
+    patch_seqs only = *seqs;                                          // the call has no rows
+    only.q_start = nullptr;
+    only.n_tokens = only.n_seqs;
+    only.max_q = 0;
+    TRY(fill_seqs(&a.seqs, &only, cache->page_size));
+    if (stride < a.seqs.max_kv || stride > ((int64_t)1 << 32) || stride % 4) return PATCH_ERR_SHAPE;
+    if (seqs->n_seqs * cache->kv_heads > (1 << 22)) return PATCH_ERR_SHAPE;
+    a.w = W;
+    a.w_out = opts->W_out;
+    a.w_stride = stride;
+    a.positions = opts->positions;
+    a.positions_out = opts->positions_out;
+    a.from = opts->from;
+    a.kv_len_out = opts->kv_len_out;
+    a.keep = (int)opts->keep;
+    a.sinks = (int)opts->sinks;
+    a.recent = (int)opts->recent;
+    launch_evict(a, static_cast<hipStream_t>(stream));
+    return launched();
+}
+
+extern "C" {
+
+patch_status patch_attention(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache* cache, void* O, int64_t o_stride,
+                             void* stream, const patch_attention_opts* opts) {
+    return attend(Q, q_stride, heads, seqs, cache, O, o_stride, stream, opts);
+}
+patch_status patch_attention4(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache4* cache, void* O, int64_t o_stride,
+                              void* stream, const patch_attention_opts* opts) {
+    return attend(Q, q_stride, heads, seqs, cache, O, o_stride, stream, opts);
+}
+size_t patch_attention_workspace_bytes(int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const patch_attention_opts* opts) {
+    return workspace_bytes(heads, seqs, cache, opts);
+}
+size_t patch_attention4_workspace_bytes(int heads, const patch_seqs* seqs, const patch_kv_cache4* cache, const patch_attention_opts* opts) {
+    return workspace_bytes(heads, seqs, cache, opts);
+}
+patch_status patch_attention_weights(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const float* lse,
+                                     const float* W, float* W_out, int64_t stride, void* stream, const patch_weights_opts* opts) {
+    return weigh(Q, q_stride, heads, seqs, cache, lse, W, W_out, stride, stream, opts);
+}
+patch_status patch_attention_weights4(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache4* cache, const float* lse,
+                                      const float* W, float* W_out, int64_t stride, void* stream, const patch_weights_opts* opts) {
+    return weigh(Q, q_stride, heads, seqs, cache, lse, W, W_out, stride, stream, opts);
+}
+patch_status patch_kv_evict(const patch_seqs* seqs, const patch_kv_cache* cache, const float* W, int64_t stride, const patch_evict_opts* opts, void* stream) {
+    return evict(seqs, cache, W, stride, opts, stream);
+}
+patch_status patch_kv_evict4(const patch_seqs* seqs, const patch_kv_cache4* cache, const float* W, int64_t stride, const patch_evict_opts* opts, void* stream) {
+    return evict(seqs, cache, W, stride, opts, stream);
 }
 
 // For tests on the host: what the kernels make of a sequence's numbers (first, n, len, pos0, bad), and of a page number.

@@ -1,0 +1,302 @@
+// How much each cached token has been attended to (patch_attention_weights):
+//
+//   w_j' = decay w_j + sum_r exp(q_r . k_j scale - lse_r)        over a key head's rows r of the call that see key j
+//
+// lse is the attention's own, so a probability needs no pass over the keys before it, and every key's sum is one workgroup's.  The product is S = Q K^T with the
+// rows on the matrix instruction's A side: a column, and so a lane, is a key, and the sum over rows stays in the lane but for its last step.
+#include <algorithm>
+
+#include "attention_kernels.h"
+
+namespace patch {
+
+constexpr int64_t kMostGroups = (int64_t)1 << 22;             // workgroups in x: far from the 2^32 threads that one launch may have there
+constexpr float kLog2e = 1.4426950408889634f;
+
+// lse of row r of a sequence's head times log2(e), plus infinity where there is nothing to add
+__device__ __forceinline__ float lse_of(const WeighArgs& a, int first, int rows, int kh, int r) {
+    if (r >= rows) return __builtin_inff();
+    const float l = as_global(a.lse)[(int64_t)(first + r / a.group) * a.heads + kh * a.group + r % a.group] * kLog2e;
+    return l == kNone ? __builtin_inff() : l;
+}
+// what is written for key j of a sequence: `sum` is of the call's rows
+__device__ __forceinline__ void put_weight(const WeighArgs& a, const Seq& q, int s, int kh, int j, float sum) {
+    if (j >= q.len) return;
+    const int64_t at = ((int64_t)s * a.cache.kv_heads + kh) * a.w_stride + j;
+    if (j < q.pos0) sum += a.decay * as_global(a.w)[at];
+    else if (a.slot_positions) as_global_out(a.slot_positions)[at] = as_global(a.positions)[q.first + (j - q.pos0)];
+    as_global_out(a.w_out)[at] = sum;
+}
+__device__ __forceinline__ float key_scale(const WeighArgs& a, int cells, int kh) {
+    return cells == kE4m3 && a.cache.k_scale ? a.scale * as_global(a.cache.k_scale)[kh] : a.scale;
+}
+__device__ __forceinline__ int page_of(const WeighArgs& a, int s, int key) {      // key: one that the sequence has
+    return page_or_none(as_global(a.seqs.table)[s * a.seqs.table_stride + (key >> a.cache.page_log2)], a.cache.n_pages);
+}
+
+// Sixteen keys of a page as the second operand of D / 32 products of 16 x 16 x 32: lane: key, eight features (in the order of query_offset).
+template <int D, int CELLS>
+struct KeyTile {
+    static constexpr int kLoads = CELLS == kBf16 ? D / 32 : CELLS == kE4m3 ? D / 64 : D < 128 ? 1 : D / 128;
+    typedef typename std::conditional<CELLS == kE2m1 && D == 64, u32x2_t, u32x4_t>::type Load;
+    Load k[kLoads];
+    uint8_t power[kLoads];
+
+    __device__ __forceinline__ void load(const CacheArgs& c, int page, int slot, int kh, int lane) {
+        const int64_t token = ((int64_t)kh << c.page_log2) + slot + (lane & 15);
+        constexpr int kBytes = CELLS == kBf16 ? 2 * D : CELLS == kE4m3 ? D : D / 2;
+        const PATCH_EP_GLOBAL uint8_t* at = as_global(c.k) + page * c.page_bytes + token * kBytes + sizeof(Load) * (lane >> 4);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) k[i] = *reinterpret_cast<const PATCH_EP_GLOBAL Load*>(at + 64 * i);
+        if constexpr (CELLS == kE2m1) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) power[i] = as_global(c.k_power)[page * c.power_bytes + token * (D / 32) + 4 * i + (D == 64 ? lane >> 5 : lane >> 4)];
+        }
+    }
+    __device__ __forceinline__ bf16x8_t operand(int i) const {
+        if constexpr (CELLS == kE2m1) return as_bf16x8(widen8_e2m1(k[i / 4][i % 4], power_of(power[i / 4])));
+        else if constexpr (CELLS == kE4m3) return as_bf16x8(widen8(k[i / 2][2 * (i % 2)], k[i / 2][2 * (i % 2) + 1]));
+        else return as_bf16x8(k[i]);
+    }
+};
+
+// Few rows (16 RB at most): each wavefront has `steps` steps of 64 keys, straight from memory into the operands' registers, the next step's on their way.
+template <int D, int RB, int CELLS>
+__global__ __launch_bounds__(256, 2) void weigh_few_kernel(const WeighArgs a, const int steps) {
+    const int s = blockIdx.y, kh = blockIdx.x % a.cache.kv_heads, lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int begin = (blockIdx.x / a.cache.kv_heads * 4 + wave) * (steps * 64);
+    const Seq q = seq_at(a.seqs, s);
+    if (q.bad || q.n == 0 || begin >= q.len) return;
+    const int end = min(q.len, begin + steps * 64), rows = min(q.n, a.seqs.max_q) * a.group, mask = (1 << a.cache.page_log2) - 1;
+    const float scale = key_scale(a, CELLS, kh);
+    bf16x8_t query[RB][D / 32];
+    float lse[RB][4];
+    int limit[RB][4];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        const int r = 16 * b + col;
+        const int64_t at = r < rows ? (int64_t)(q.first + r / a.group) * a.q_stride + (int64_t)(kh * a.group + r % a.group) * D : 0;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            u32x4_t v = {0, 0, 0, 0};
+            if (r < rows) v = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(a.Q) + at + query_offset<D, CELLS>(i, g));
+            query[b][i] = as_bf16x8(v);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = 16 * b + 4 * g + e;
+            lse[b][e] = lse_of(a, q.first, rows, kh, row);
+            limit[b][e] = row < rows ? q.pos0 + row / a.group + 1 : 0;
+        }
+    }
+    typedef KeyTile<D, CELLS> Tile;
+    const auto ask = [&](Tile (&to)[4], int (&page)[4], int step) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int key = step + 16 * t;
+            page[t] = key < q.len ? page_of(a, s, key) : -1;
+            to[t].load(a.cache, max(page[t], 0), key & mask, kh, lane);
+        }
+    };
+    Tile keys[4];
+    int page[4];
+    ask(keys, page, begin);
+    for (int step = begin; step < end; step += 64) {
+        f32x4_t x[RB][4];
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) x[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                const bf16x8_t k = keys[t].operand(i);
+#pragma unroll
+                for (int b = 0; b < RB; ++b) x[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(query[b][i], k, x[b][t], 0, 0, 0);
+            }
+        int now[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) now[t] = page[t];
+        if (step + 64 < end) ask(keys, page, step + 64);
+        float mine = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int key = step + 16 * t + col;
+            float sum = 0.f;
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][t][e], scale, -lse[b][e]));
+                    sum += key < limit[b][e] ? p : 0.f;
+                }
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (now[t] < 0) sum = __builtin_nanf("");
+            if (g == t) mine = sum;
+        }
+        put_weight(a, q, s, kh, step + lane, mine);
+    }
+}
+
+// Many rows: a workgroup's wavefronts have 32 KB keys each, in registers as operands, and the rows come through LDS for all of them, 64 at a time, the next ones
+// on their way through registers meanwhile.
+template <int D>
+struct RowTilesLds {
+    u32x4_t q[2][64 * D / 8];
+    float lse[2][64];
+    int limit[2][64];
+};
+
+template <int D, int KB, int CELLS>
+__device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, int block, RowTilesLds<D>& sh) {
+    constexpr int kRowLoads = D / 8, kRowStep = 256 / kRowLoads, kEach = 64 / kRowStep, kKeys = 32 * KB;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Seq q = seq_at(a.seqs, s);
+    if (q.bad || q.n == 0 || block >= q.len) return;
+    const int rows = min(q.n, a.seqs.max_q) * a.group, key0 = block + wave * kKeys, mask = (1 << a.cache.page_log2) - 1;
+    const float scale = key_scale(a, CELLS, kh);
+    bf16x8_t k[KB][D / 16];
+    bool none[KB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+        const int key = key0 + 32 * b + col;
+        int page = -1;
+        if (key < q.len) page = page_of(a, s, key);
+        none[b] = page < 0;
+        const int64_t token = ((int64_t)kh << a.cache.page_log2) + (key & mask);
+        const PATCH_EP_GLOBAL uint8_t* at = as_global(a.cache.k) + max(page, 0) * a.cache.page_bytes;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            const int64_t cell = token * D + 16 * i + 8 * h;
+            if constexpr (CELLS == kBf16) {
+                k[b][i] = as_bf16x8(*reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(at + 2 * cell));
+            } else if constexpr (CELLS == kE4m3) {
+                const u32x2_t w = *reinterpret_cast<const PATCH_EP_GLOBAL u32x2_t*>(at + cell);
+                k[b][i] = as_bf16x8(widen8(w[0], w[1]));
+            } else {
+                const uint32_t w = *reinterpret_cast<const PATCH_EP_GLOBAL uint32_t*>(at + cell / 2);
+                const uint32_t power = as_global(a.cache.k_power)[max(page, 0) * a.cache.power_bytes + cell / 32];
+                k[b][i] = as_bf16x8(widen8_e2m1(w, power_of(power)));
+            }
+        }
+    }
+    float sum[KB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) sum[b] = 0.f;
+
+    const int row = tid / kRowLoads, chunk = tid % kRowLoads;
+    u32x4_t regs[kEach];
+    float lse_reg = 0.f;
+    const auto ask = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int r = min(tile + row + i * kRowStep, rows - 1);
+            regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(a.Q) + (int64_t)(q.first + r / a.group) * a.q_stride +
+                                                                        (int64_t)(kh * a.group + r % a.group) * D + 8 * chunk);
+        }
+        if (tid < 64) lse_reg = lse_of(a, q.first, rows, kh, tile + tid);
+    };
+    const auto put = [&](int tile, int buffer) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) sh.q[buffer][chunk_at<D / 8>(row + i * kRowStep, chunk)] = regs[i];
+        if (tid < 64) {
+            sh.lse[buffer][tid] = lse_reg;
+            sh.limit[buffer][tid] = tile + tid < rows ? q.pos0 + (tile + tid) / a.group + 1 : 0;
+        }
+    };
+    // rows in front see none of the keys
+    const int64_t first_row = (int64_t)max(block - q.pos0, 0) * a.group;
+    const int first = (int)(first_row & ~63);
+    if (first < rows) {
+        ask(first);
+        put(first, 0);
+    }
+    __syncthreads();
+    int buffer = 0;
+    for (int tile = first; tile < rows; tile += 64, buffer ^= 1) {
+        const bool more = tile + 64 < rows;
+        if (more) ask(tile + 64);
+        const int last_limit = q.pos0 + min(tile + 63, rows - 1) / a.group + 1;
+        if (key0 < last_limit && key0 < q.len) {
+            const bool ragged = tile + 64 > rows || key0 + kKeys > q.pos0 + tile / a.group + 1;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f32x16_t x[KB];
+#pragma unroll
+                for (int b = 0; b < KB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[b][e] = 0.f;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const bf16x8_t query = as_bf16x8(sh.q[buffer][chunk_at<D / 8>(32 * half + col, 2 * i + h)]);
+#pragma unroll
+                    for (int b = 0; b < KB; ++b) x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(query, k[b][i], x[b], 0, 0, 0);
+                }
+#pragma unroll
+                for (int e4 = 0; e4 < 4; ++e4) {
+                    const int r = 32 * half + 8 * e4 + 4 * h;
+                    const f32x4_t l = *reinterpret_cast<const f32x4_t*>(&sh.lse[buffer][r]);
+#pragma unroll
+                    for (int b = 0; b < KB; ++b)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][4 * e4 + e], scale, -l[e]));
+                            if (ragged) p = key0 + 32 * b + col < sh.limit[buffer][r + e] ? p : 0.f;
+                            sum[b] += p;
+                        }
+                }
+            }
+        }
+        if (more) put(tile + 64, buffer ^ 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+        float w = sum[b] + __shfl_xor(sum[b], 32);
+        if (none[b]) w = __builtin_nanf("");
+        if (h == 0) put_weight(a, q, s, kh, key0 + 32 * b + col, w);
+    }
+}
+
+template <int D, int KB, int CELLS>
+__global__ __launch_bounds__(256, 2) void weigh_tiles_kernel(const WeighArgs a) {
+    __shared__ RowTilesLds<D> sh;
+    // the keys that most rows see come first
+    for (int64_t block = blockIdx.x / a.cache.kv_heads * (128 * KB); block < a.seqs.max_kv; block += gridDim.x / a.cache.kv_heads * (128 * KB))
+        weigh_tiles<D, KB, CELLS>(a, blockIdx.y, blockIdx.x % a.cache.kv_heads, (int)block, sh);
+}
+
+template <int D, int CELLS>
+static void launch_weigh_of(const WeighArgs& a, hipStream_t stream) {
+    const int64_t rows = (int64_t)a.seqs.max_q * a.group, units = (int64_t)a.seqs.n_seqs * a.cache.kv_heads;
+    const unsigned heads = (unsigned)a.cache.kv_heads, seqs = (unsigned)a.seqs.n_seqs;
+    if (rows <= 32) {
+        const int64_t all = (a.seqs.max_kv + 63) / 64;
+        const int64_t most = std::max<int64_t>(kMostGroups / heads, 1);             // workgroups of a head
+        const int steps = (int)std::max(std::min<int64_t>(std::max<int64_t>(all * units / 2048, 1), 8), (all + 4 * most - 1) / (4 * most));
+        const unsigned blocks = (unsigned)((all + 4 * steps - 1) / (4 * steps));
+        if (rows <= 16) weigh_few_kernel<D, 1, CELLS><<<dim3(blocks * heads, seqs), 256, 0, stream>>>(a, steps);
+        else weigh_few_kernel<D, 2, CELLS><<<dim3(blocks * heads, seqs), 256, 0, stream>>>(a, steps);
+        return;
+    }
+    constexpr int KB = 1;
+    const int64_t blocks = std::min<int64_t>((a.seqs.max_kv + 128 * KB - 1) / (128 * KB), std::max<int64_t>(kMostGroups / heads, 1));
+    weigh_tiles_kernel<D, KB, CELLS><<<dim3((unsigned)blocks * heads, seqs), 256, 0, stream>>>(a);
+}
+template <int CELLS>
+static void launch_weigh_cells(const WeighArgs& a, hipStream_t stream) {
+    if (a.cache.head_dim == 64) launch_weigh_of<64, CELLS>(a, stream);
+    else if (a.cache.head_dim == 128) launch_weigh_of<128, CELLS>(a, stream);
+    else launch_weigh_of<256, CELLS>(a, stream);
+}
+void launch_weigh(const WeighArgs& a, hipStream_t stream) {
+    if (a.cache.cells == kE2m1) launch_weigh_cells<kE2m1>(a, stream);
+    else if (a.cache.cells == kE4m3) launch_weigh_cells<kE4m3>(a, stream);
+    else launch_weigh_cells<kBf16>(a, stream);
+}
+
+}  // namespace patch

@@ -32,7 +32,7 @@ __device__ __forceinline__ void append_v_tile(const RopeArgs& a, int tile, int k
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
         const int i = i0 + n * kStep;
-        if (a.cache.e4m3) {
+        if (a.cache.cells == kE4m3) {
             const uint32_t u = pack_e4m3(x[n], scale);
 #pragma unroll
             for (int e = 0; e < 4; ++e) sh_v[d + e][i] = (u >> (8 * e)) & 0xFFu;
@@ -54,7 +54,7 @@ __device__ __forceinline__ void append_v_tile(const RopeArgs& a, int tile, int k
 #pragma unroll 4
     for (int f = threadIdx.x / (kTurn / 8); f < D; f += 256 / (kTurn / 8)) {
         const int64_t cell = slot + ((int64_t)f << a.cache.page_log2);
-        if (a.cache.e4m3) {
+        if (a.cache.cells == kE4m3) {
             if (whole) {
                 u32x2_t w;
 #pragma unroll
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
         const int64_t cells = (int64_t)at[u] << a.cache.page_log2;       // those of the heads in front, over D
         if (kind[u] == 1) {
             uint8_t* base = a.cache.k + page * a.cache.page_bytes;
-            if (a.cache.e4m3) {
+            if (a.cache.cells == kE4m3) {
                 const float scale = a.cache.k_scale ? as_global(a.cache.k_scale)[at[u]] : 1.f;
                 base += (cells + slot) * D;
                 *reinterpret_cast<PATCH_EP_GLOBAL uint32_t*>(as_global_out(base) + i0) = pack_e4m3(y0, scale);
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
         } else {                                                 // V: feature-major, the token's values are a page apart
             uint8_t* base = a.cache.v + page * a.cache.page_bytes;
             const int p = a.cache.page_log2;
-            if (a.cache.e4m3) {
+            if (a.cache.cells == kE4m3) {
                 const float scale = a.cache.v_scale ? as_global(a.cache.v_scale)[at[u]] : 1.f;
                 const uint32_t u0 = pack_e4m3(y0, scale), u1 = pack_e4m3(y1, scale);
                 base += cells * D + slot;
