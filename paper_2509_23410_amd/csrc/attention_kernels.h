@@ -136,28 +136,14 @@ __device__ __forceinline__ bool any_infinite(const u32x4_t& v) {      // or NaN
     return any;
 }
 
-__device__ __forceinline__ float bf16_value(const void* base, int64_t i) {
-    return __uint_as_float((uint32_t)reinterpret_cast<const PATCH_EP_GLOBAL uint16_t*>(as_global(static_cast<const uint8_t*>(base)))[i] << 16);
+template <bool E4M3>
+__device__ __forceinline__ float cell_value(const uint8_t* base, int64_t i) {
+    if (E4M3) return __builtin_amdgcn_cvt_f32_fp8((int)as_global(base)[i], 0);
+    return __uint_as_float((uint32_t)reinterpret_cast<const PATCH_EP_GLOBAL uint16_t*>(as_global(base))[i] << 16);
 }
-// Feature d of K and of V of the token in slot `slot` of a page (without the factor that a head of e4m3 has).
-template <int D, int CELLS>
-__device__ __forceinline__ float k_value(const AttnArgs& a, int64_t page, int kh, int slot, int d) {
-    const int64_t token = ((int64_t)kh << a.cache.page_log2) + slot;
-    const uint8_t* base = a.cache.k + page * a.cache.page_bytes;
-    if constexpr (CELLS == kE2m1)
-        return e2m1_value(as_global(base)[token * (D / 2) + d / 2] >> (4 * (d % 2)), as_global(a.cache.k_power)[page * a.cache.power_bytes + token * (D / 32) + d / 32]);
-    else if constexpr (CELLS == kE4m3) return __builtin_amdgcn_cvt_f32_fp8((int)as_global(base)[token * D + d], 0);
-    else return bf16_value(base, token * D + d);
-}
-template <int D, int CELLS>
-__device__ __forceinline__ float v_value(const AttnArgs& a, int64_t page, int kh, int slot, int d) {
-    const int p = a.cache.page_log2;
-    const uint8_t* base = a.cache.v + page * a.cache.page_bytes;
-    if constexpr (CELLS == kE2m1)
-        return e2m1_value(as_global(base)[(((int64_t)kh * (D / 2) + d / 2) << p) + slot] >> (4 * (d % 2)),
-                          as_global(a.cache.v_power)[page * a.cache.power_bytes + (((int64_t)kh * (D / 32) + d / 32) << p) + slot]);
-    else if constexpr (CELLS == kE4m3) return __builtin_amdgcn_cvt_f32_fp8((int)as_global(base)[(((int64_t)kh * D + d) << p) + slot], 0);
-    else return bf16_value(base, (((int64_t)kh * D + d) << p) + slot);
+// The same of a cell of 4 bits, which is half of byte `byte` and has power `power`.
+__device__ __forceinline__ float cell4_value(const uint8_t* base, const uint8_t* powers, int64_t byte, int64_t power, int half) {
+    return e2m1_value(as_global(base)[byte] >> (4 * half), as_global(powers)[power]);
 }
 
 // One row by one wavefront, key by key and with no key that the row does not see.  In the products of the kernels below a row has 0 times the values of the
@@ -175,17 +161,27 @@ __device__ __forceinline__ void attend_row_alone(const AttnArgs& a, const Span& 
     if (CELLS == kE4m3 && a.cache.v_scale) v_scale = as_global(a.cache.v_scale)[kh];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        q[e] = bf16_value(a.Q, token * a.q_stride + (int64_t)head * D + lane * E + e);
+        q[e] = cell_value<false>(reinterpret_cast<const uint8_t*>(a.Q), token * a.q_stride + (int64_t)head * D + lane * E + e);
         acc[e] = 0.f;
     }
 #pragma unroll 1
     for (int key = max(p.begin, p.key0); key < min(p.end, limit); ++key) {
         const int id = p.bad ? -1 : page_or_none(as_global(a.seqs.table)[p.table + (key >> a.cache.page_log2)], a.cache.n_pages);
         float s = 0.f, v[E];
+        const int64_t cells = (int64_t)kh << a.cache.page_log2;
+        const uint8_t *k_page = a.cache.k + max(id, 0) * a.cache.page_bytes, *v_page = a.cache.v + max(id, 0) * a.cache.page_bytes;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            s += q[e] * k_value<D, CELLS>(a, max(id, 0), kh, key & mask, lane * E + e);
-            v[e] = v_value<D, CELLS>(a, max(id, 0), kh, key & mask, lane * E + e);
+            const int d = lane * E + e;
+            if constexpr (CELLS == kE2m1) {
+                const int64_t powers = max(id, 0) * a.cache.power_bytes;
+                s += q[e] * cell4_value(k_page, a.cache.k_power + powers, ((cells + (key & mask)) * D + d) / 2, ((cells + (key & mask)) * D + d) / 32, d % 2);
+                v[e] = cell4_value(v_page, a.cache.v_power + powers, cells * (D / 2) + ((int64_t)(d / 2) << a.cache.page_log2) + (key & mask),
+                                   cells * (D / 32) + ((int64_t)(d / 32) << a.cache.page_log2) + (key & mask), d % 2);
+            } else {
+                s += q[e] * cell_value<CELLS == kE4m3>(k_page, (cells + (key & mask)) * D + d);
+                v[e] = cell_value<CELLS == kE4m3>(v_page, cells * D + ((int64_t)d << a.cache.page_log2) + (key & mask));
+            }
         }
 #pragma unroll
         for (int x = 1; x < 64; x <<= 1) s += __shfl_xor(s, x);
@@ -688,9 +684,10 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
     // staging: each thread's key rows of K (one a load), and keys of V (the same ones for all its loads, of different features)
     const int page_mask = (1 << a.cache.page_log2) - 1;
     const int k_row = tid / kRowLoads, v_row = tid / kKeyLoads, v_key = (tid % kKeyLoads) * kRunKeys;
-    constexpr int kRowStep = kThreads / kRowLoads, kFeatureStep = kThreads / kKeyLoads, kKeyBytes = 16 * D / kCells, kBytes = 16 / kRunKeys;
+    constexpr int kRowStep = kThreads / kRowLoads, kFeatureStep = kThreads / kKeyLoads, kBytes = 16 / kRunKeys;
     const uint32_t page_bytes = (uint32_t)a.cache.page_bytes;
-    const uint8_t* k_base = a.cache.k + (((int64_t)kh * kKeyBytes) << a.cache.page_log2) + (tid % kRowLoads) * 16;
+    constexpr int kTokenLoads = CELLS == kE2m1 ? D / 32 : D, kTokenBytes = CELLS == kE2m1 ? 16 : kBytes;      // of K, and bytes of one
+    const uint8_t* k_base = a.cache.k + ((((int64_t)kh * kTokenLoads) << a.cache.page_log2) + (tid % kRowLoads) * (CELLS == kE2m1 ? 1 : kCells)) * kTokenBytes;
     const uint8_t* v_base = a.cache.v + (((int64_t)kh * (D / kRows) + half * (DV / kRows) + v_row) << a.cache.page_log2) * kBytes;
     const uint32_t v_step = (uint32_t)(kFeatureStep * kBytes) << a.cache.page_log2;
     u32x4_t k_regs[kEachK], v_regs[kEachV];
@@ -705,7 +702,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
             for (int i = 0; i < kEachK; ++i) {
                 const int key = tile + k_row + i * kRowStep, page = pages[key >> a.cache.page_log2];
                 k_none[i] = page < 0;
-                k_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(k_base) + ((uint64_t)(uint32_t)max(page, 0) * page_bytes + (uint32_t)((key & page_mask) * kKeyBytes)));
+                k_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(k_base) + ((uint64_t)(uint32_t)max(page, 0) * page_bytes + (uint32_t)((key & page_mask) * (kTokenLoads * kTokenBytes))));
                 if constexpr (CELLS == kE2m1)
                     k_powers[i] = as_global(a.cache.k_power)[max(page, 0) * a.cache.power_bytes + (((int64_t)kh << a.cache.page_log2) + (key & page_mask)) * (D / 32) + tid % kRowLoads];
             }
@@ -746,23 +743,28 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
         if (kLoadsV >= kThreads || tid < kLoadsV) {
 #pragma unroll
             for (int i = 0; i < kEachV; ++i) {
-                const auto put = [&](int feature, int b, u32x4_t v) {
-                    if (any_none && v_none) v = u32x4_t{0, 0, 0, 0};
-                    if (edge) v &= keys_in(tile + v_key + 8 * b, p.key0, p.key1);        // cells that no key is in
-                    if (!seen_by_all) infinite |= any_infinite(v);
-                    sh.v[buffer][chunk_at<kTile / 8>(feature, v_key / 8 + b)] = v;
-                };
+                if constexpr (CELLS == kE2m1) {
 #pragma unroll
-                for (int b = 0; b < kRunKeys / 8; ++b) {
-                    const int row = v_row + i * kFeatureStep;
-                    if constexpr (CELLS == kE2m1) {
+                    for (int b = 0; b < kRunKeys / 8; ++b) {
                         const Two8 t = turn8_e2m1(v_regs[i][2 * b], v_regs[i][2 * b + 1], v_powers[i][2 * b], v_powers[i][2 * b + 1]);
-                        put(2 * row, b, t.even);
-                        put(2 * row + 1, b, t.odd);
-                    } else if constexpr (CELLS == kE4m3) {
-                        put(row, b, widen8(v_regs[i][2 * b], v_regs[i][2 * b + 1]));
-                    } else {
-                        put(row, b, v_regs[i]);
+#pragma unroll
+                        for (int odd = 0; odd < 2; ++odd) {
+                            u32x4_t v = odd ? t.odd : t.even;
+                            if (any_none && v_none) v = u32x4_t{0, 0, 0, 0};
+                            if (edge) v &= keys_in(tile + v_key + 8 * b, p.key0, p.key1);
+                            if (!seen_by_all) infinite |= any_infinite(v);
+                            sh.v[buffer][chunk_at<kTile / 8>(2 * (v_row + i * kFeatureStep) + odd, v_key / 8 + b)] = v;
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < kParts; ++b) {
+                        u32x4_t v = v_regs[i];
+                        if constexpr (CELLS == kE4m3) v = widen8(v_regs[i][2 * b], v_regs[i][2 * b + 1]);
+                        if (any_none && v_none) v = u32x4_t{0, 0, 0, 0};
+                        if (edge) v &= keys_in(tile + v_key + 8 * b, p.key0, p.key1);        // cells that no key is in
+                        if (!seen_by_all) infinite |= any_infinite(v);
+                        sh.v[buffer][chunk_at<kTile / 8>(v_row + i * kFeatureStep, v_key / 8 + b)] = v;
                     }
                 }
             }
