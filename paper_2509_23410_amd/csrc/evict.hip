@@ -11,222 +11,478 @@ namespace patch {
 
 // Larger: heavier.  NaN: 0; always staying: all ones (a number's is at most 0xFF800000, that of infinity).
 __device__ __forceinline__ uint32_t rank_of(float w, bool always) {
-    const uint32_t u = __float_as_uint(w);
-    if (always) return 0xFFFFFFFFu;
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0u;
-    if ((u & 0x7FFFFFFFu) == 0u) return 0x80000000u;             // both zeros
-    return u >> 31 ? ~u : u | 0x80000000u;
+    const int u = __float_as_int(w + 0.f);                       // both zeros are one
+    const uint32_t r = w != w ? 0u : (uint32_t)(u ^ (u >> 31 | INT32_MIN));
+    return always ? 0xFFFFFFFFu : r;
 }
-
-constexpr int kSelect = 1024;          // threads
-constexpr int kChunk = 4 * kSelect;    // slots at a time
-
-struct SelectLds {
-    int count[2048];
-    int wave[16][4];
-    int movers[2 * kChunk];            // slots behind the budget whose tokens stay, as a ring
+// Positions that always stay: those below `sinks`, and if `any` those from `last` on.
+struct Always {
+    int sinks, last;
+    bool any;
+    __device__ __forceinline__ bool operator()(int p) const { return p < sinks || (any && p >= last); }
 };
 
-// Sums of x over the threads in front of this one, and of all.
-__device__ __forceinline__ int before_me(int x, int (*wave)[4], int which, int* total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    int sum = x;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const int other = __shfl_up(sum, m);
-        if (lane >= m) sum += other;
-    }
-    if (lane == 63) wave[w][which] = sum;
-    __syncthreads();
-    int front = 0, all = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int n = wave[i][which];
-        front += i < w ? n : 0;
-        all += n;
-    }
-    __syncthreads();
-    *total = all;
-    return front + sum - x;
+// Sums over the lanes up to this one: of its row of 16, and of all.
+__device__ __forceinline__ uint32_t row_sums(uint32_t x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);      // lanes 1, 2, 4 and 8 in front
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    return x;
+}
+__device__ __forceinline__ uint32_t lane_sums(uint32_t x) {
+    x = row_sums(x);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);     // the last lane of rows 0 and 2 to rows 1 and 3, then that of row 1 to rows 2 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
 }
 
-__global__ __launch_bounds__(kSelect) void evict_select_kernel(const EvictArgs a) {
-    __shared__ SelectLds sh;
-    const int kh = blockIdx.x % a.cache.kv_heads, s = blockIdx.x / a.cache.kv_heads, tid = threadIdx.x, keep = a.keep;
+constexpr int kThreads = 1024, kWaves = kThreads / 64;   // (of 256 threads 64 sequences of 4097 slots, 8 key heads, took 24 us for 20)
+constexpr int kStrip = 4 * kThreads;                     // slots that they have four each of, side by side
+
+// The ranks of J strips of slots from `base` on: strip j's slots 4 tid .. 4 tid + 3 in r[j].
+template <int J>
+struct Ranks {
+    uint32_t r[J][4];
+    u32x4_t at[J], asked[J];           // positions, and weights as they are loaded (rows of both are a multiple of four apart)
+    int base, begin, len;              // there are those in [begin, len)
+
+    __device__ __forceinline__ int slot(int j) const { return base + j * kStrip + 4 * (int)threadIdx.x; }
+    __device__ __forceinline__ void ask(const float* w, const int32_t* pos, int first, int length) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int i = first + j * kStrip + 4 * (int)threadIdx.x;
+            asked[j] = u32x4_t{0, 0, 0, 0};
+            if (i < length) asked[j] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(w) + i);
+            if (pos && i < length) at[j] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(pos) + i);
+        }
+    }
+    // the largest position of those asked for
+    __device__ __forceinline__ int newest(int length) const {
+        int top = INT32_MIN;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (j * kStrip + 4 * (int)threadIdx.x + e < length) top = max(top, (int)at[j][e]);
+        return top;
+    }
+    // what was asked for
+    __device__ __forceinline__ void take(const int32_t* pos, int first, int lowest, int length, const Always& always) {
+        base = first;
+        begin = lowest;
+        len = length;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[j][e] = rank_of(__uint_as_float(asked[j][e]), always(pos ? (int)at[j][e] : slot(j) + e));
+    }
+    // whether strip j is all there, and else a bit for each of the thread's slots that is
+    __device__ __forceinline__ bool whole(int j) const { return base + j * kStrip >= begin && base + (j + 1) * kStrip <= len; }
+    __device__ __forceinline__ uint32_t bits(int j) const {
+        uint32_t b = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b |= slot(j) + e >= begin && slot(j) + e < len ? 1u << e : 0u;
+        return b;
+    }
+    // f(rank) of those that there are
+    template <typename F>
+    __device__ __forceinline__ void each(const F& f) const {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (whole(j)) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f(r[j][e]);
+            } else {
+                const uint32_t b = bits(j);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (b >> e & 1) f(r[j][e]);
+            }
+        }
+    }
+};
+
+// Histograms are four side by side, of every fourth lane each: an atomic add takes as long as its most frequent address has lanes.
+constexpr int kCopies = 4, kBins = 2048;
+
+template <int J, int RING>
+struct SelectLds {
+    int count[kBins * kCopies];
+    uint32_t strip[J][kWaves];         // counts of a strip's wavefronts
+    int wave[kWaves], found[3];
+    int movers[RING];                  // slots behind the budget whose tokens stay
+};
+
+// front[j] = the sums of x[j] (two counts of 16 bits) over the threads in front of this one in strip j, total[j] = of the whole strip
+template <int J>
+__device__ __forceinline__ void before_me(const uint32_t (&x)[J], uint32_t (*strip)[kWaves], uint32_t (&front)[J], uint32_t (&total)[J]) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const uint32_t sum = lane_sums(x[j]);
+        if (lane == 63) strip[j][w] = sum;
+        front[j] = sum - x[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j0 = 0; j0 < J; j0 += 4) {                          // the wavefronts of four strips at a time, one a lane
+        const uint32_t n = j0 + (lane >> 4) < J ? strip[j0 + (lane >> 4)][lane & 15] : 0, sum = row_sums(n);
+#pragma unroll
+        for (int j = j0; j < J && j < j0 + 4; ++j) {
+            front[j] += __builtin_amdgcn_readlane(sum - n, 16 * (j - j0) + w);
+            total[j] = __builtin_amdgcn_readlane(sum, 16 * (j - j0) + 15);
+        }
+    }
+    __syncthreads();
+}
+// The sum of x over all threads, added to by each wavefront.
+__device__ __forceinline__ int sum_of_all(int x, int* wave) {
+    const uint32_t sum = lane_sums((uint32_t)x);
+    if ((threadIdx.x & 63) == 63) wave[threadIdx.x >> 6] = (int)sum;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) all += wave[i];
+    __syncthreads();
+    return all;
+}
+
+// Slots of a block in their order: which stay, and the ranks of holes and of movers among their like.  `left` of the border's stay, the first ones, `ties` of which have
+// been seen; some: not all of them do.
+template <int J>
+struct Block {
+    uint32_t stays[J], front[J], total[J];      // a bit each; holes in the low half, movers in the high one: in front in the strip, and in all of it
+
+    __device__ __forceinline__ void look(const Ranks<J>& k, uint32_t (*strip)[kWaves], int keep, uint32_t border, bool some, int left, int* ties) {
+        uint32_t there[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            there[j] = k.whole(j) ? 15u : k.bits(j);
+            stays[j] = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) stays[j] |= k.r[j][e] >= border ? 1u << e : 0u;
+            stays[j] &= there[j];
+        }
+        uint32_t n[J];
+        if (some) {
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                n[j] = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) n[j] += k.r[j][e] == border && (there[j] >> e & 1);
+            }
+            before_me<J>(n, strip, front, total);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                int tie = *ties + (int)front[j];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (k.r[j][e] == border && (there[j] >> e & 1) && tie++ >= left) stays[j] &= ~(1u << e);
+                *ties += (int)total[j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int within = min(max(keep - k.slot(j), 0), 4);             // of the thread's four
+            const uint32_t low = (1u << within) - 1;
+            n[j] = __builtin_popcount(there[j] & ~stays[j] & low) + (__builtin_popcount(stays[j] & ~low) << 16);
+        }
+        before_me<J>(n, strip, front, total);
+    }
+    __device__ __forceinline__ int holes() const {
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) n += (int)(total[j] & 0xFFFFu);
+        return n;
+    }
+    // the movers' slots into a ring, `movers` of them are in it
+    template <int RING>
+    __device__ __forceinline__ void collect(const Ranks<J>& k, int keep, int* ring, int* movers) const {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            int at = *movers + (int)(front[j] >> 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (k.slot(j) + e >= keep && (stays[j] >> e & 1)) ring[at++ % RING] = k.slot(j) + e;
+            *movers += (int)(total[j] >> 16);
+        }
+    }
+    // what is in the slots within the budget afterwards; `holes` were in front
+    template <int RING>
+    __device__ __forceinline__ void fill(const Ranks<J>& k, int keep, const int* ring, int* holes, int32_t* from) const {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            int hole = *holes + (int)(front[j] & 0xFFFFu);
+            typedef int Four32 __attribute__((ext_vector_type(4), aligned(4)));
+            const int i = k.slot(j);
+            Four32 came = {i, i + 1, i + 2, i + 3};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < keep && !(stays[j] >> e & 1)) came[e] = ring[hole++ % RING];
+            if (i + 3 < keep) {
+                *reinterpret_cast<PATCH_EP_GLOBAL Four32*>(as_global_out(from) + i) = came;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < keep) as_global_out(from)[i + e] = came[e];
+            }
+            *holes += (int)(total[j] & 0xFFFFu);
+        }
+    }
+};
+
+// One workgroup for each sequence and key head.  WHOLE: its ranks stay in registers (J strips hold all of them), else they are read again in each pass.
+template <int J, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs a) {
+    constexpr int B = WHOLE ? J : 2;                            // strips of a block in the last pass
+    constexpr int kRing = WHOLE ? J * kStrip / 2 : 2 * B * kStrip;              // of `len` slots at most half move
+    __shared__ alignas(16) SelectLds<B, kRing> sh;
+    const int kh = blockIdx.x % a.cache.kv_heads, s = blockIdx.x / a.cache.kv_heads, tid = threadIdx.x, lane = tid & 63, keep = a.keep;
     const int64_t unit = (int64_t)s * a.cache.kv_heads + kh;
     const Seq q = seq_at(a.seqs, s);
     int32_t* from = a.from + unit * keep;
     const int len = q.bad ? 0 : q.len;
     if (len <= keep) {
-        for (int i = tid; i < keep; i += kSelect) as_global_out(from)[i] = i < len ? i : -1;
+        for (int i = tid; i < keep; i += kThreads) as_global_out(from)[i] = i < len ? i : -1;
         return;
     }
     const float* w = a.w + unit * a.w_stride;
     const int32_t* pos = a.positions ? a.positions + unit * a.w_stride : nullptr;
-    // the largest position
-    int newest = len - 1;
+    Ranks<J> ranks;
+    if (WHOLE) ranks.ask(w, pos, 0, len);
+    int newest = len - 1;                                        // the largest position
     if (pos) {
         newest = INT32_MIN;
-        for (int i = tid; i < len; i += kSelect) newest = max(newest, as_global(pos)[i]);
+        if (WHOLE) newest = ranks.newest(len);
+        else
+            for (int i = 4 * tid; i < len; i += 4 * kStrip) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int at = min(i + j * kStrip, (len - 1) & ~3);
+                    const u32x4_t x = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(pos) + at);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (at + e < len) newest = max(newest, (int)x[e]);
+                }
+            }
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) newest = max(newest, __shfl_xor(newest, m));
-        if ((tid & 63) == 0) sh.wave[tid >> 6][0] = newest;
+        if (lane == 0) sh.wave[tid >> 6] = newest;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) newest = max(newest, sh.wave[i][0]);
-        __syncthreads();
+        for (int i = 0; i < kWaves; ++i) newest = max(newest, sh.wave[i]);
     }
-    const int64_t recent = (int64_t)newest - a.recent;
-    const auto rank_at = [&](int i) {
-        const int p = pos ? as_global(pos)[i] : i;
-        return rank_of(as_global(w)[i], p < a.sinks || p > recent);
+    const Always always = {a.sinks, (int)max((int64_t)newest - a.recent + 1, (int64_t)INT32_MIN), a.recent > 0};
+    if (WHOLE) ranks.take(pos, 0, 0, len, always);
+    // f() with the ranks of the slots [0, length), J strips at a time, the next ones on their way
+    const auto stream = [&](int length, const auto& f) {
+        ranks.ask(w, pos, 0, length);
+        for (int first = 0; first < length; first += J * kStrip) {
+            ranks.take(pos, first, 0, length, always);
+            if (first + J * kStrip < length) ranks.ask(w, pos, first + J * kStrip, length);
+            f();
+        }
     };
-    // the border: `border` is the rank of the last that stays, `left` how many of that rank do
+    // the border: `border` is the rank of the last that stays, `left` how many of that rank do, `same` how many have it
     uint32_t border = 0;
-    int left = keep;
+    int left = keep, same = 0;
+    int candidates = -1;                                         // of the first digit, where the list has room for them: other digits are looked up there
     for (int digit = 0; digit < 3; ++digit) {
-        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : 2048;
-        for (int i = tid; i < bins; i += kSelect) sh.count[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < len; i += kSelect) {
-            const uint32_t r = rank_at(i);
-            if (digit == 0 || r >> (shift + (digit == 1 ? 11 : 10)) == border >> (shift + (digit == 1 ? 11 : 10))) atomicAdd(&sh.count[(r >> shift) & (bins - 1)], 1);
+        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? kBins / 2 : kBins, above = digit == 0 ? 31 : digit == 1 ? 21 : 10;
+        for (int i = tid; i < bins; i += kThreads) *reinterpret_cast<u32x4_t*>(&sh.count[kCopies * i]) = u32x4_t{0, 0, 0, 0};
+        if (!WHOLE && digit == 1 && same <= kRing) {
+            candidates = same;
+            if (tid == 0) sh.found[2] = 0;
         }
         __syncthreads();
-        // bins from the largest on, two a thread: the one in which the sum reaches `left`
-        const int top = bins - 1 - 2 * tid, n0 = top > 0 ? sh.count[top] : 0, n1 = top > 0 ? sh.count[top - 1] : 0;
-        int total;
-        const int front = before_me(n0 + n1, sh.wave, 0, &total);
-        if (front < left && left <= front + n0 + n1) {
-            const bool second = front + n0 < left;
-            sh.wave[0][1] = top - (second ? 1 : 0);
-            sh.wave[0][2] = left - front - (second ? n0 : 0);
+        const auto count = [&](uint32_t r) {
+            if (digit == 0 || r >> above == border >> above) atomicAdd(&sh.count[kCopies * ((r >> shift) & (bins - 1)) + (lane & (kCopies - 1))], 1);
+        };
+        if (WHOLE) {
+            ranks.each(count);
+        } else if (candidates < 0) {
+            stream(len, [&] { ranks.each(count); });
+        } else if (digit == 1) {
+            stream(len, [&] {
+                int mine = 0;
+                ranks.each([&](uint32_t r) { mine += r >> above == border >> above; });
+                const int upto = (int)lane_sums((uint32_t)mine);
+                int at = 0;
+                if (lane == 63 && upto) at = atomicAdd(&sh.found[2], upto);
+                at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
+                if (mine)
+                    ranks.each([&](uint32_t r) {
+                        if (r >> above != border >> above) return;
+                        sh.movers[at++] = (int)r;
+                        count(r);
+                    });
+            });
+        } else {
+            for (int i = tid; i < candidates; i += kThreads) count((uint32_t)sh.movers[i]);
         }
         __syncthreads();
-        border |= (uint32_t)sh.wave[0][1] << shift;
-        left = sh.wave[0][2];
+        // bins from the largest on, kBins / kThreads a thread (the last digit: half of them): the one in which the sum reaches `left`
+        const auto in_bin = [&](int i) {
+            const u32x4_t n = *reinterpret_cast<const u32x4_t*>(&sh.count[kCopies * i]);
+            return (int)(n[0] + n[1] + n[2] + n[3]);
+        };
+        const int each = bins / kThreads, top = bins - 1 - each * tid;
+        int n[kBins / kThreads], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kBins / kThreads; ++i) {
+            n[i] = i < each ? in_bin(top - i) : 0;
+            sum += n[i];
+        }
+        const int upto = (int)lane_sums((uint32_t)sum);
+        if (lane == 63) sh.wave[tid >> 6] = upto;
+        __syncthreads();
+        int front = upto - sum;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) front += i < tid >> 6 ? sh.wave[i] : 0;
+        if (front < left && left <= front + sum) {
+#pragma unroll
+            for (int i = 0; i < kBins / kThreads; ++i) {
+                if (front < left && left <= front + n[i]) {
+                    sh.found[0] = top - i;
+                    sh.found[1] = left - front;
+                }
+                front += n[i];
+            }
+        }
+        __syncthreads();
+        border |= (uint32_t)sh.found[0] << shift;
+        left = sh.found[1];
+        same = in_bin(sh.found[0]);
         __syncthreads();
     }
-    // slots in their order: which of the border's stay, the ranks of holes and of movers
-    int ties = 0, holes = 0, movers = 0, ahead = keep;           // behind the budget `ahead` slots have been looked at
-    int ties_ahead;
-    {
-        int mine = 0;
-        for (int i = tid; i < keep; i += kSelect) mine += rank_at(i) == border;
-        before_me(mine, sh.wave, 0, &ties_ahead);
-    }
-    for (int chunk = 0; chunk < keep; chunk += kChunk) {
-        bool stays[4];
-        int equal[4], n = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = chunk + 4 * tid + e;
-            const uint32_t r = i < keep ? rank_at(i) : 0xFFFFFFFFu;
-            equal[e] = i < keep && r == border;
-            stays[e] = i >= keep || r > border;
-            n += equal[e];
+
+    const bool some = left < same;                               // not all of the border's stay: those in the lowest slots
+    int holes = 0, movers = 0, ties = 0;
+    if constexpr (WHOLE) {
+        Block<J> block;
+        block.look(ranks, sh.strip, keep, border, some, left, &ties);
+        block.template collect<kRing>(ranks, keep, sh.movers, &movers);
+        __syncthreads();
+        block.template fill<kRing>(ranks, keep, sh.movers, &holes, from);
+    } else {
+        int ties_behind = 0;                                     // the border's behind the budget come after all of those within it
+        if (some) {
+            int mine = 0;
+            stream(keep, [&] { ranks.each([&](uint32_t r) { mine += r == border; }); });
+            ties_behind = sum_of_all(mine, sh.wave);
         }
-        int total;
-        int tie = ties + before_me(n, sh.wave, 0, &total);
-        ties += total;
-        n = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (equal[e]) stays[e] = tie++ < left;
-            n += !stays[e];
-        }
-        int hole = holes + before_me(n, sh.wave, 1, &total);
-        holes += total;
-        // as many movers as these holes take
-        while (movers < holes && ahead < len) {
-            int m = 0, eq = 0;
-            bool goes[4], same[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = ahead + 4 * tid + e;
-                const uint32_t r = i < len ? rank_at(i) : 0u;
-                same[e] = i < len && r == border;
-                goes[e] = i < len && r > border;
-                eq += same[e];
+        // as many movers as the holes so far take
+        Ranks<B> here, behind;
+        Block<B> block, other;
+        int ahead = keep & ~3;
+        behind.ask(w, pos, ahead, len);
+        here.ask(w, pos, 0, keep);
+        for (int first = 0; first < keep; first += B * kStrip) {
+            here.take(pos, first, 0, keep, always);
+            if (first + B * kStrip < keep) here.ask(w, pos, first + B * kStrip, keep);
+            block.look(here, sh.strip, keep, border, some, left, &ties);
+            while (movers < holes + block.holes() && ahead < len) {
+                behind.take(pos, ahead, keep, len, always);
+                ahead += B * kStrip;
+                if (ahead < len) behind.ask(w, pos, ahead, len);
+                other.look(behind, sh.strip, keep, border, some, left, &ties_behind);
+                other.template collect<kRing>(behind, keep, sh.movers, &movers);
             }
-            int tied = ties_ahead + before_me(eq, sh.wave, 2, &total);
-            ties_ahead += total;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (same[e]) goes[e] = tied++ < left;
-                m += goes[e];
-            }
-            int at = movers + before_me(m, sh.wave, 3, &total);
-            movers += total;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (goes[e]) sh.movers[at++ % (2 * kChunk)] = ahead + 4 * tid + e;
-            ahead += kChunk;
+            __syncthreads();
+            block.template fill<kRing>(here, keep, sh.movers, &holes, from);
             __syncthreads();
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = chunk + 4 * tid + e;
-            if (i < keep) as_global_out(from)[i] = stays[e] ? i : sh.movers[hole % (2 * kChunk)];
-            hole += !stays[e];
-        }
-        __syncthreads();
     }
 }
 
-// Cells to where `from` says: 64 slots of a sequence's head by a workgroup, lanes beside each other with slots beside each other.
+// Cells to where `from` says, by workgroups of 256 slots of a sequence's head, and the weights and positions of all its slots.
 template <int CELL>     // bytes of a cell of V's rows: 2, 1 (e4m3), 0: pairs of 4 bits and powers
 __device__ __forceinline__ void move_slots(const EvictArgs& a, int s, int kh, int first) {
-    __shared__ int sh_to[64], sh_from[64], sh_n;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, slot = first + lane;
+    __shared__ int sh_to[256], sh_from[256], sh_n[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, slot = first + tid;
     const int64_t unit = (int64_t)s * a.cache.kv_heads + kh;
     const int came = slot < a.keep ? as_global(a.from)[unit * a.keep + slot] : -1;
-    if (wave == 0) {
-        if (came >= 0) {
-            const int64_t to = unit * a.w_stride + slot, at = unit * a.w_stride + came;
-            if (a.w_out) as_global_out(a.w_out)[to] = as_global(a.w)[at];
-            if (a.positions_out) as_global_out(a.positions_out)[to] = a.positions ? as_global(a.positions)[at] : came;
-        }
-        const bool moves = came >= 0 && came != slot;
-        const uint64_t all = __ballot(moves);
-        if (moves) {
-            const int i = __builtin_popcountll(all & ((1ull << lane) - 1));
-            sh_to[i] = slot;
-            sh_from[i] = came;
-        }
-        if (lane == 0) sh_n = __builtin_popcountll(all);
+    if (came >= 0) {
+        const int64_t to = unit * a.w_stride + slot, at = unit * a.w_stride + came;
+        if (a.w_out) as_global_out(a.w_out)[to] = as_global(a.w)[at];
+        if (a.positions_out) as_global_out(a.positions_out)[to] = a.positions ? as_global(a.positions)[at] : came;
+    }
+    const bool moves = came >= 0 && came != slot;
+    const uint64_t all = __ballot(moves);
+    if (lane == 0) sh_n[wave] = __builtin_popcountll(all);
+    __syncthreads();
+    int n = 0, mine = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        mine += i < wave ? sh_n[i] : 0;
+        n += sh_n[i];
+    }
+    if (n == 0) return;
+    const int p = a.cache.page_log2, mask = (1 << p) - 1, D = a.cache.head_dim;
+    if (moves) {
+        mine += __builtin_popcountll(all & ((1ull << lane) - 1));
+        sh_to[mine] = slot;
+        sh_from[mine] = came;
     }
     __syncthreads();
-    const int n = sh_n, p = a.cache.page_log2, mask = (1 << p) - 1, D = a.cache.head_dim;
-    if (lane >= n) return;
-    const int to = sh_to[lane], at = sh_from[lane];
     const PATCH_EP_GLOBAL int32_t* table = as_global(a.seqs.table) + s * a.seqs.table_stride;
-    const int64_t dst = page_or_none(table[to >> p], a.cache.n_pages), src = page_or_none(table[at >> p], a.cache.n_pages);
-    if (dst < 0 || src < 0) return;
-    const int64_t head = (int64_t)kh << p;
-    const auto copy = [&](auto* base, int64_t stride, int64_t goal, int64_t source) {    // of one element
-        typedef typename std::remove_reference<decltype(*base)>::type T;
-        const uint8_t* b = reinterpret_cast<const uint8_t*>(base);
-        *reinterpret_cast<PATCH_EP_GLOBAL T*>(as_global_out(const_cast<uint8_t*>(b)) + dst * stride + goal) =
-            *reinterpret_cast<const PATCH_EP_GLOBAL T*>(as_global(b) + src * stride + source);
-    };
-    const int bytes = CELL == 0 ? D / 2 : D * CELL;
-    const int64_t k_to = (head + (to & mask)) * bytes, k_at = (head + (at & mask)) * bytes;
-    for (int c = 16 * wave; c < bytes; c += 64) copy(reinterpret_cast<u32x4_t*>(a.cache.k), a.cache.page_bytes, k_to + c, k_at + c);
-    const int features = CELL == 0 ? D / 2 : D;
-    const int64_t row = (int64_t)kh * features;
-    for (int d = wave; d < features; d += 4) {
-        const int64_t f = (row + d) << p;
-        if constexpr (CELL == 2) copy(reinterpret_cast<uint16_t*>(a.cache.v), a.cache.page_bytes, 2 * (f + (to & mask)), 2 * (f + (at & mask)));
-        else copy(a.cache.v, a.cache.page_bytes, f + (to & mask), f + (at & mask));
-    }
-    if constexpr (CELL == 0) {
-        const int powers = D / 32;
-        for (int b = wave; b < powers; b += 4) {
-            copy(a.cache.k_power, a.cache.power_bytes, (head + (to & mask)) * powers + b, (head + (at & mask)) * powers + b);
-            const int64_t f = ((int64_t)kh * powers + b) << p;
-            copy(a.cache.v_power, a.cache.power_bytes, f + (to & mask), f + (at & mask));
+    // pages of a move, -1: not to be followed
+    const auto page = [&](int slot_of) { return (int64_t)page_or_none(table[slot_of >> p], a.cache.n_pages); };
+    constexpr int kBatch = 8;                                    // loads that a thread has on their way: a store may not pass a load that could be of its cell
+    // rows of K: 16-byte pieces of a row by neighbouring threads
+    const int bytes = CELL == 0 ? D / 2 : D * CELL, pieces = __builtin_ctz(bytes / 16);
+    for (int item = tid; item < n << pieces; item += 256 * kBatch) {
+        u32x4_t x[kBatch];
+        int64_t goal[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int i = item + 256 * b;
+            goal[b] = -1;
+            if (i >= n << pieces) continue;
+            const int to = sh_to[i >> pieces], at = sh_from[i >> pieces], c = 16 * (i & ((1 << pieces) - 1));
+            const int64_t dst = page(to), src = page(at);
+            if (dst < 0 || src < 0) continue;
+            goal[b] = dst * a.cache.page_bytes + (((int64_t)kh << p) + (to & mask)) * bytes + c;
+            x[b] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(a.cache.k) + src * a.cache.page_bytes + (((int64_t)kh << p) + (at & mask)) * bytes + c);
         }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+            if (goal[b] >= 0) *reinterpret_cast<PATCH_EP_GLOBAL u32x4_t*>(as_global_out(a.cache.k) + goal[b]) = x[b];
+    }
+    // V, and powers: a cell of a row for neighbouring moves by neighbouring threads, the rows of a token by others
+    const int side = n <= 1 ? 0 : n > 32 ? 6 : 32 - __builtin_clz(n - 1);        // 2^side moves at a time
+    const auto cells = [&](auto* base, int64_t stride, int rows, bool by_token) {
+        typedef typename std::remove_reference<decltype(*base)>::type T;
+        const uint8_t* buffer = reinterpret_cast<const uint8_t*>(base);
+        for (int m0 = 0; m0 < n; m0 += 1 << side) {
+            const int m = m0 + (tid & ((1 << side) - 1));
+            if (m >= n) continue;
+            const int to = sh_to[m], at = sh_from[m];
+            const int64_t dst = page(to), src = page(at);
+            if (dst < 0 || src < 0) continue;
+            // element `r` of a token: rows side by side for a token, or tokens side by side for a row
+            const auto place = [&](int64_t id, int of, int r) {
+                const int64_t in_page = by_token ? (((int64_t)kh << p) + (of & mask)) * rows + r : (((int64_t)kh * rows + r) << p) + (of & mask);
+                return id * stride + in_page * (int64_t)sizeof(T);
+            };
+            const int step = 256 >> side;
+            for (int r0 = tid >> side; r0 < rows; r0 += step * kBatch) {
+                T x[kBatch];
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b)
+                    if (r0 + b * step < rows) x[b] = *reinterpret_cast<const PATCH_EP_GLOBAL T*>(as_global(buffer) + place(src, at, r0 + b * step));
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b)
+                    if (r0 + b * step < rows) *reinterpret_cast<PATCH_EP_GLOBAL T*>(as_global_out(const_cast<uint8_t*>(buffer)) + place(dst, to, r0 + b * step)) = x[b];
+            }
+        }
+    };
+    if constexpr (CELL == 2) cells(reinterpret_cast<uint16_t*>(a.cache.v), a.cache.page_bytes, D, false);
+    else cells(a.cache.v, a.cache.page_bytes, CELL == 0 ? D / 2 : D, false);
+    if constexpr (CELL == 0) {
+        cells(a.cache.k_power, a.cache.power_bytes, D / 32, true);
+        cells(a.cache.v_power, a.cache.power_bytes, D / 32, false);
     }
 }
 
@@ -238,16 +494,18 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a) {
         as_global_out(a.kv_len_out)[s] = len > a.seqs.max_kv ? len : max(min(len, a.keep), 0);
     }
     const int most = min(a.keep, a.seqs.max_kv);                 // (behind that nobody has tokens)
-    for (int first = blockIdx.x / a.cache.kv_heads * 64; first < most; first += gridDim.x / a.cache.kv_heads * 64) {
+    for (int first = blockIdx.x / a.cache.kv_heads * 256; first < most; first += gridDim.x / a.cache.kv_heads * 256) {
         move_slots<CELL>(a, s, kh, first);
         __syncthreads();
     }
 }
 
 void launch_evict(const EvictArgs& a, hipStream_t stream) {
-    const unsigned heads = (unsigned)a.cache.kv_heads;
-    evict_select_kernel<<<(unsigned)a.seqs.n_seqs * heads, kSelect, 0, stream>>>(a);
-    const unsigned chunks = (unsigned)std::min<int64_t>(((int64_t)std::min(a.keep, std::max(a.seqs.max_kv, 1)) + 63) / 64, std::max((1u << 22) / heads, 1u));
+    const unsigned heads = (unsigned)a.cache.kv_heads, units = (unsigned)a.seqs.n_seqs * heads;
+    if (a.seqs.max_kv <= 2 * kStrip) evict_select_kernel<2, true><<<units, kThreads, 0, stream>>>(a);
+    else if (a.seqs.max_kv <= 4 * kStrip) evict_select_kernel<4, true><<<units, kThreads, 0, stream>>>(a);
+    else evict_select_kernel<4, false><<<units, kThreads, 0, stream>>>(a);
+    const unsigned chunks = (unsigned)std::min<int64_t>(((int64_t)std::min(a.keep, std::max(a.seqs.max_kv, 1)) + 255) / 256, std::max((1u << 22) / heads, 1u));
     const dim3 grid(chunks * heads, (unsigned)a.seqs.n_seqs);
     if (a.cache.cells == kBf16) evict_move_kernel<2><<<grid, 256, 0, stream>>>(a);
     else if (a.cache.cells == kE4m3) evict_move_kernel<1><<<grid, 256, 0, stream>>>(a);
