@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256, 2) void weigh_few_kernel(const WeighArgs a, co
     }
 }
 
-// Many rows: a workgroup's wavefronts have 32 KB keys each, in registers as operands, and the rows come through LDS for all of them, 64 at a time, the next ones
+// Many rows: a workgroup's wavefronts have 32 keys each, in registers as operands, and the rows come through LDS for all of them, 64 at a time, the next ones
 // on their way through registers meanwhile.
 template <int D>
 struct RowTilesLds {
@@ -150,124 +150,141 @@ struct RowTilesLds {
     int limit[2][64];
 };
 
-template <int D, int KB, int CELLS>
+template <int D, int NW, int CELLS>
 __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, int block, RowTilesLds<D>& sh) {
-    constexpr int kRowLoads = D / 8, kRowStep = 256 / kRowLoads, kEach = 64 / kRowStep, kKeys = 32 * KB;
+    constexpr int kThreads = 64 * NW, kRowLoads = D / 8, kRowStep = kThreads / kRowLoads, kEach = 64 / kRowStep, kKeys = 32;
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Seq q = seq_at(a.seqs, s);
     if (q.bad || q.n == 0 || block >= q.len) return;
     const int rows = min(q.n, a.seqs.max_q) * a.group, key0 = block + wave * kKeys, mask = (1 << a.cache.page_log2) - 1;
     const float scale = key_scale(a, CELLS, kh);
-    bf16x8_t k[KB][D / 16];
-    bool none[KB];
-#pragma unroll
-    for (int b = 0; b < KB; ++b) {
-        const int key = key0 + 32 * b + col;
+    bf16x8_t k[D / 16];
+    bool none;
+    {
+        const int key = key0 + col;
         int page = -1;
         if (key < q.len) page = page_of(a, s, key);
-        none[b] = page < 0;
+        none = page < 0;
         const int64_t token = ((int64_t)kh << a.cache.page_log2) + (key & mask);
         const PATCH_EP_GLOBAL uint8_t* at = as_global(a.cache.k) + max(page, 0) * a.cache.page_bytes;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
             const int64_t cell = token * D + 16 * i + 8 * h;
             if constexpr (CELLS == kBf16) {
-                k[b][i] = as_bf16x8(*reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(at + 2 * cell));
+                k[i] = as_bf16x8(*reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(at + 2 * cell));
             } else if constexpr (CELLS == kE4m3) {
                 const u32x2_t w = *reinterpret_cast<const PATCH_EP_GLOBAL u32x2_t*>(at + cell);
-                k[b][i] = as_bf16x8(widen8(w[0], w[1]));
+                k[i] = as_bf16x8(widen8(w[0], w[1]));
             } else {
                 const uint32_t w = *reinterpret_cast<const PATCH_EP_GLOBAL uint32_t*>(at + cell / 2);
                 const uint32_t power = as_global(a.cache.k_power)[max(page, 0) * a.cache.power_bytes + cell / 32];
-                k[b][i] = as_bf16x8(widen8_e2m1(w, power_of(power)));
+                k[i] = as_bf16x8(widen8_e2m1(w, power_of(power)));
             }
         }
     }
-    float sum[KB];
-#pragma unroll
-    for (int b = 0; b < KB; ++b) sum[b] = 0.f;
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 
     const int row = tid / kRowLoads, chunk = tid % kRowLoads;
+    // rows in front see none of the keys
+    const int first = (int)((int64_t)max(block - q.pos0, 0) * a.group & ~(int64_t)63);
+    // A row's place follows from that of the row 64 in front of it: so many elements, and if it is not in the same token's heads any more so many more.
+    const int heads64 = 64 % a.group;
+    const int64_t step = 64 / a.group * a.q_stride + heads64 * D, wrap = a.q_stride - (int64_t)a.group * D;
+    int64_t at[kEach];
+    int head[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int r = first + row + i * kRowStep;
+        head[i] = r % a.group;
+        at[i] = r / a.group * a.q_stride + head[i] * D;
+    }
+    const PATCH_EP_GLOBAL uint16_t* queries = as_global(a.Q) + (int64_t)q.first * a.q_stride + (int64_t)kh * a.group * D + 8 * chunk;
+    // the first wavefront has their lse, too
+    int lse_token = (first + lane) / a.group, lse_head = (first + lane) % a.group;
     u32x4_t regs[kEach];
     float lse_reg = 0.f;
+    int limit_reg = 0;
     const auto ask = [&](int tile) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int r = min(tile + row + i * kRowStep, rows - 1);
-            regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(a.Q) + (int64_t)(q.first + r / a.group) * a.q_stride +
-                                                                        (int64_t)(kh * a.group + r % a.group) * D + 8 * chunk);
+            regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(queries + (tile + row + i * kRowStep < rows ? at[i] : 0));     // (no row: any, its limit is 0)
+            head[i] += heads64;
+            at[i] += step + (head[i] >= a.group ? wrap : 0);
+            head[i] -= head[i] >= a.group ? a.group : 0;
         }
-        if (tid < 64) lse_reg = lse_of(a, q.first, rows, kh, tile + tid);
+        if (wave == 0) {
+            const bool there = tile + lane < rows;
+            lse_reg = as_global(a.lse)[(int64_t)(q.first + (there ? lse_token : 0)) * a.heads + kh * a.group + lse_head];
+            limit_reg = there ? q.pos0 + lse_token + 1 : 0;
+            lse_head += heads64;
+            lse_token += 64 / a.group + (lse_head >= a.group);
+            lse_head -= lse_head >= a.group ? a.group : 0;
+        }
     };
-    const auto put = [&](int tile, int buffer) {
+    const auto put = [&](int buffer) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) sh.q[buffer][chunk_at<D / 8>(row + i * kRowStep, chunk)] = regs[i];
-        if (tid < 64) {
-            sh.lse[buffer][tid] = lse_reg;
-            sh.limit[buffer][tid] = tile + tid < rows ? q.pos0 + (tile + tid) / a.group + 1 : 0;
+        if (wave == 0) {
+            sh.lse[buffer][lane] = lse_reg == kNone ? __builtin_inff() : lse_reg * kLog2e;
+            sh.limit[buffer][lane] = limit_reg;
         }
     };
-    // rows in front see none of the keys
-    const int64_t first_row = (int64_t)max(block - q.pos0, 0) * a.group;
-    const int first = (int)(first_row & ~63);
     if (first < rows) {
         ask(first);
-        put(first, 0);
+        put(0);
     }
+    // the keys are there: else the first product of each step waits for them, and with them for the rows that were asked for since (125 us for 82)
+    __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();
     int buffer = 0;
     for (int tile = first; tile < rows; tile += 64, buffer ^= 1) {
         const bool more = tile + 64 < rows;
         if (more) ask(tile + 64);
-        const int last_limit = q.pos0 + min(tile + 63, rows - 1) / a.group + 1;
-        if (key0 < last_limit && key0 < q.len) {
-            const bool ragged = tile + 64 > rows || key0 + kKeys > q.pos0 + tile / a.group + 1;
+        // limits never fall from row to row, and those of no rows are 0
+        const int lowest = __builtin_amdgcn_readfirstlane(sh.limit[buffer][0]), highest = __builtin_amdgcn_readfirstlane(sh.limit[buffer][min(rows - tile, 64) - 1]);
+        if (key0 < highest) {
+            const bool ragged = tile + 64 > rows || key0 + kKeys > lowest;       // not every row is there and sees all of the keys
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                f32x16_t x[KB];
+                f32x16_t x;
 #pragma unroll
-                for (int b = 0; b < KB; ++b)
+                for (int e = 0; e < 16; ++e) x[e] = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) x[b][e] = 0.f;
+                for (int i = 0; i < D / 16; ++i)
+                    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh.q[buffer][chunk_at<D / 8>(32 * half + col, 2 * i + h)]), k[i], x, 0, 0, 0);
+                const auto add = [&](auto masked) {
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const bf16x8_t query = as_bf16x8(sh.q[buffer][chunk_at<D / 8>(32 * half + col, 2 * i + h)]);
-#pragma unroll
-                    for (int b = 0; b < KB; ++b) x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(query, k[b][i], x[b], 0, 0, 0);
-                }
-#pragma unroll
-                for (int e4 = 0; e4 < 4; ++e4) {
-                    const int r = 32 * half + 8 * e4 + 4 * h;
-                    const f32x4_t l = *reinterpret_cast<const f32x4_t*>(&sh.lse[buffer][r]);
-#pragma unroll
-                    for (int b = 0; b < KB; ++b)
+                    for (int e4 = 0; e4 < 4; ++e4) {
+                        const int r = 32 * half + 8 * e4 + 4 * h;
+                        const f32x4_t l = *reinterpret_cast<const f32x4_t*>(&sh.lse[buffer][r]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][4 * e4 + e], scale, -l[e]));
-                            if (ragged) p = key0 + 32 * b + col < sh.limit[buffer][r + e] ? p : 0.f;
-                            sum[b] += p;
+                            float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * e4 + e], scale, -l[e]));
+                            if constexpr (decltype(masked)::value) p = key0 + col < sh.limit[buffer][r + e] ? p : 0.f;
+                            sum[e] += p;
                         }
-                }
+                    }
+                };
+                if (ragged) add(std::true_type{});
+                else add(std::false_type{});
             }
         }
-        if (more) put(tile + 64, buffer ^ 1);
+        if (more) put(buffer ^ 1);
         __syncthreads();
     }
-#pragma unroll
-    for (int b = 0; b < KB; ++b) {
-        float w = sum[b] + __shfl_xor(sum[b], 32);
-        if (none[b]) w = __builtin_nanf("");
-        if (h == 0) put_weight(a, q, s, kh, key0 + 32 * b + col, w);
-    }
+    float w = sum[0] + sum[1] + (sum[2] + sum[3]);
+    w += __shfl_xor(w, 32);
+    if (none) w = __builtin_nanf("");
+    if (h == 0) put_weight(a, q, s, kh, key0 + col, w);
 }
 
-template <int D, int KB, int CELLS>
-__global__ __launch_bounds__(256, 2) void weigh_tiles_kernel(const WeighArgs a) {
+template <int D, int NW, int CELLS>
+__global__ __launch_bounds__(64 * NW, 2) void weigh_tiles_kernel(const WeighArgs a) {
     __shared__ RowTilesLds<D> sh;
     // the keys that most rows see come first
-    for (int64_t block = blockIdx.x / a.cache.kv_heads * (128 * KB); block < a.seqs.max_kv; block += gridDim.x / a.cache.kv_heads * (128 * KB))
-        weigh_tiles<D, KB, CELLS>(a, blockIdx.y, blockIdx.x % a.cache.kv_heads, (int)block, sh);
+    for (int64_t block = blockIdx.x / a.cache.kv_heads * (32 * NW); block < a.seqs.max_kv; block += gridDim.x / a.cache.kv_heads * (32 * NW))
+        weigh_tiles<D, NW, CELLS>(a, blockIdx.y, blockIdx.x % a.cache.kv_heads, (int)block, sh);
 }
 
 template <int D, int CELLS>
@@ -283,9 +300,9 @@ static void launch_weigh_of(const WeighArgs& a, hipStream_t stream) {
         else weigh_few_kernel<D, 2, CELLS><<<dim3(blocks * heads, seqs), 256, 0, stream>>>(a, steps);
         return;
     }
-    constexpr int KB = 1;
-    const int64_t blocks = std::min<int64_t>((a.seqs.max_kv + 128 * KB - 1) / (128 * KB), std::max<int64_t>(kMostGroups / heads, 1));
-    weigh_tiles_kernel<D, KB, CELLS><<<dim3((unsigned)blocks * heads, seqs), 256, 0, stream>>>(a);
+    constexpr int NW = 4;
+    const int64_t blocks = std::min<int64_t>((a.seqs.max_kv + 32 * NW - 1) / (32 * NW), std::max<int64_t>(kMostGroups / heads, 1));
+    weigh_tiles_kernel<D, NW, CELLS><<<dim3((unsigned)blocks * heads, seqs), 64 * NW, 0, stream>>>(a);
 }
 template <int CELLS>
 static void launch_weigh_cells(const WeighArgs& a, hipStream_t stream) {
