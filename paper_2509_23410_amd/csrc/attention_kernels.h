@@ -309,7 +309,7 @@ struct StepKeys<D, RB, kE2m1> {
     static_assert(HB == 2, "16 keys of V to a load");
     typedef typename std::conditional<D == 64, u32x2_t, u32x4_t>::type KLoad;
     KLoad k[HB][2][kLoads];
-    uint8_t k_power[HB][2][kLoads];
+    uint32_t k_power[HB][2][kLoads];
     u32x4_t v[D / 32], v_power[D / 32];
 
     static __device__ __forceinline__ int k_key(int lane) { return kRun * ((lane & 15) >> 2); }
@@ -637,8 +637,10 @@ template <int D, int NW, int CELLS>
 __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, int kh, int half, int first_row, TilesLds<D, NW>& sh) {
     constexpr int kTile = TilesLds<D, NW>::kTile, kBlocks = kTile / 32;        // keys at a time, as 32 to an instruction
     constexpr int DV = TilesLds<D, NW>::DV;
-    constexpr int kThreads = 64 * NW, kCells = CELLS == kE2m1 ? 32 : CELLS == kE4m3 ? 16 : 8;      // of a 16-byte load
+    constexpr int kThreads = 64 * NW, kLoad = CELLS == kE2m1 && NW == 8 ? 8 : 16;                  // bytes of a load: every thread has one
+    constexpr int kCells = CELLS == kE2m1 ? 2 * kLoad : CELLS == kE4m3 ? 16 : 8;
     constexpr int kRows = CELLS == kE2m1 ? 2 : 1, kRunKeys = kCells / kRows;   // a load of V: so many features of so many keys
+    typedef typename std::conditional<kLoad == 8, u32x2_t, u32x4_t>::type Load;
     constexpr int kLoadsK = kTile * D / kCells, kEachK = (kLoadsK + kThreads - 1) / kThreads;
     constexpr int kLoadsV = kTile * DV / kCells, kEachV = (kLoadsV + kThreads - 1) / kThreads;
     constexpr int kRowLoads = D / kCells, kKeyLoads = kTile / kRunKeys;        // of a key, of a feature
@@ -684,15 +686,15 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
     // staging: each thread's key rows of K (one a load), and keys of V (the same ones for all its loads, of different features)
     const int page_mask = (1 << a.cache.page_log2) - 1;
     const int k_row = tid / kRowLoads, v_row = tid / kKeyLoads, v_key = (tid % kKeyLoads) * kRunKeys;
-    constexpr int kRowStep = kThreads / kRowLoads, kFeatureStep = kThreads / kKeyLoads, kBytes = 16 / kRunKeys;
+    constexpr int kRowStep = kThreads / kRowLoads, kFeatureStep = kThreads / kKeyLoads, kBytes = kLoad / kRunKeys;
     const uint32_t page_bytes = (uint32_t)a.cache.page_bytes;
-    constexpr int kTokenLoads = CELLS == kE2m1 ? D / 32 : D, kTokenBytes = CELLS == kE2m1 ? 16 : kBytes;      // of K, and bytes of one
+    constexpr int kTokenLoads = CELLS == kE2m1 ? D / kCells : D, kTokenBytes = CELLS == kE2m1 ? kLoad : kBytes;      // of K, and bytes of one
     const uint8_t* k_base = a.cache.k + ((((int64_t)kh * kTokenLoads) << a.cache.page_log2) + (tid % kRowLoads) * (CELLS == kE2m1 ? 1 : kCells)) * kTokenBytes;
     const uint8_t* v_base = a.cache.v + (((int64_t)kh * (D / kRows) + half * (DV / kRows) + v_row) << a.cache.page_log2) * kBytes;
     const uint32_t v_step = (uint32_t)(kFeatureStep * kBytes) << a.cache.page_log2;
-    u32x4_t k_regs[kEachK], v_regs[kEachV];
+    Load k_regs[kEachK], v_regs[kEachV];
     uint8_t k_powers[kEachK];                                                   // (of 4-bit cells)
-    u32x4_t v_powers[kEachV];
+    Load v_powers[kEachV];
     bool k_none[kEachK], v_none, any_none = false;                              // keys without a page
     int window = p.begin, fewest_of_all = 0;
     const auto ask_keys = [&](int tile) {
@@ -702,9 +704,9 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
             for (int i = 0; i < kEachK; ++i) {
                 const int key = tile + k_row + i * kRowStep, page = pages[key >> a.cache.page_log2];
                 k_none[i] = page < 0;
-                k_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(k_base) + ((uint64_t)(uint32_t)max(page, 0) * page_bytes + (uint32_t)((key & page_mask) * (kTokenLoads * kTokenBytes))));
+                k_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL Load*>(as_global(k_base) + ((uint64_t)(uint32_t)max(page, 0) * page_bytes + (uint32_t)((key & page_mask) * (kTokenLoads * kTokenBytes))));
                 if constexpr (CELLS == kE2m1)
-                    k_powers[i] = as_global(a.cache.k_power)[max(page, 0) * a.cache.power_bytes + (((int64_t)kh << a.cache.page_log2) + (key & page_mask)) * (D / 32) + tid % kRowLoads];
+                    k_powers[i] = as_global(a.cache.k_power)[max(page, 0) * a.cache.power_bytes + (((int64_t)kh << a.cache.page_log2) + (key & page_mask)) * (D / 32) + tid % kRowLoads * kCells / 32];
             }
         }
         if (kLoadsV >= kThreads || tid < kLoadsV) {
@@ -712,11 +714,11 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
             v_none = page < 0;
             const PATCH_EP_GLOBAL uint8_t* at = as_global(v_base) + ((uint64_t)(uint32_t)max(page, 0) * page_bytes + (uint32_t)((key & page_mask) * kBytes));
 #pragma unroll
-            for (int i = 0; i < kEachV; ++i) v_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(at + i * v_step);
+            for (int i = 0; i < kEachV; ++i) v_regs[i] = *reinterpret_cast<const PATCH_EP_GLOBAL Load*>(at + i * v_step);
             if constexpr (CELLS == kE2m1) {
 #pragma unroll
                 for (int i = 0; i < kEachV; ++i)
-                    v_powers[i] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(
+                    v_powers[i] = *reinterpret_cast<const PATCH_EP_GLOBAL Load*>(
                         as_global(a.cache.v_power) + max(page, 0) * a.cache.power_bytes +
                         (((int64_t)kh * (D / 32) + (half * (DV / 2) + v_row + i * kFeatureStep) / 16) << a.cache.page_log2) + (key & page_mask));
             }
@@ -732,7 +734,8 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
                 const int at = k_row + i * kRowStep, row = (at & ~31) | key_row(at & 31);
 #pragma unroll
                 for (int b = 0; b < kParts; ++b) {
-                    u32x4_t k = k_regs[i];
+                    u32x4_t k;
+                    if constexpr (CELLS == kBf16) k = k_regs[i];
                     if constexpr (CELLS == kE4m3) k = widen8(k_regs[i][2 * b], k_regs[i][2 * b + 1]);
                     if constexpr (CELLS == kE2m1) k = widen8_e2m1(k_regs[i][b], power_of(k_powers[i]));
                     if (any_none && k_none[i]) k = u32x4_t{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};     // a page that is not there: NaN scores

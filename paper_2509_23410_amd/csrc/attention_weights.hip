@@ -19,13 +19,12 @@ __device__ __forceinline__ float lse_of(const WeighArgs& a, int first, int rows,
     const float l = as_global(a.lse)[(int64_t)(first + r / a.group) * a.heads + kh * a.group + r % a.group] * kLog2e;
     return l == kNone ? __builtin_inff() : l;
 }
-// what is written for key j of a sequence: `sum` is of the call's rows
-__device__ __forceinline__ void put_weight(const WeighArgs& a, const Seq& q, int s, int kh, int j, float sum) {
+// what is written for key j of a sequence, whose head's weights begin at `weights`: `sum` is of the call's rows, `old` what was there for a key that is not new
+__device__ __forceinline__ void put_weight(const WeighArgs& a, const Seq& q, int64_t weights, int j, float sum, float old) {
     if (j >= q.len) return;
-    const int64_t at = ((int64_t)s * a.cache.kv_heads + kh) * a.w_stride + j;
-    if (j < q.pos0) sum += a.decay * as_global(a.w)[at];
-    else if (a.slot_positions) as_global_out(a.slot_positions)[at] = as_global(a.positions)[q.first + (j - q.pos0)];
-    as_global_out(a.w_out)[at] = sum;
+    if (j < q.pos0) sum += a.decay * old;
+    else if (a.slot_positions) as_global_out(a.slot_positions)[weights + j] = as_global(a.positions)[q.first + (j - q.pos0)];
+    as_global_out(a.w_out)[weights + j] = sum;
 }
 __device__ __forceinline__ float key_scale(const WeighArgs& a, int cells, int kh) {
     return cells == kE4m3 && a.cache.k_scale ? a.scale * as_global(a.cache.k_scale)[kh] : a.scale;
@@ -91,53 +90,58 @@ __global__ __launch_bounds__(256, 2) void weigh_few_kernel(const WeighArgs a, co
         }
     }
     typedef KeyTile<D, CELLS> Tile;
-    const auto ask = [&](Tile (&to)[4], int (&page)[4], int step) {
+    const int64_t weights = ((int64_t)s * a.cache.kv_heads + kh) * a.w_stride;
+    // Pages of 64 times 16 keys, one a lane: a step's are known before it is asked for.
+    for (int window = begin; window < end; window += 1024) {
+        int ids = -1;
+        if (window + 16 * lane < end) ids = page_of(a, s, window + 16 * lane);
+        Tile keys[4];
+        float old = 0.f;
+        const auto ask = [&](int step) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int key = step + 16 * t;
-            page[t] = key < q.len ? page_of(a, s, key) : -1;
-            to[t].load(a.cache, max(page[t], 0), key & mask, kh, lane);
-        }
-    };
-    Tile keys[4];
-    int page[4];
-    ask(keys, page, begin);
-    for (int step = begin; step < end; step += 64) {
-        f32x4_t x[RB][4];
-#pragma unroll
-        for (int b = 0; b < RB; ++b)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) x[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                const bf16x8_t k = keys[t].operand(i);
-#pragma unroll
-                for (int b = 0; b < RB; ++b) x[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(query[b][i], k, x[b][t], 0, 0, 0);
+            for (int t = 0; t < 4; ++t) {
+                const int key = step + 16 * t;
+                keys[t].load(a.cache, max(__builtin_amdgcn_readlane(ids, (key - window) >> 4), 0), key & mask, kh, lane);
             }
-        int now[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) now[t] = page[t];
-        if (step + 64 < end) ask(keys, page, step + 64);
-        float mine = 0.f;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int key = step + 16 * t + col;
-            float sum = 0.f;
+            if (step + lane < q.pos0) old = as_global(a.w)[weights + step + lane];
+        };
+        ask(window);
+        const int stop = min(end, window + 1024);
+        for (int step = window; step < stop; step += 64) {
+            f32x4_t x[RB][4];
 #pragma unroll
             for (int b = 0; b < RB; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][t][e], scale, -lse[b][e]));
-                    sum += key < limit[b][e] ? p : 0.f;
+                for (int t = 0; t < 4; ++t) x[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const bf16x8_t k = keys[t].operand(i);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) x[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(query[b][i], k, x[b][t], 0, 0, 0);
                 }
-            sum += __shfl_xor(sum, 16);
-            sum += __shfl_xor(sum, 32);
-            if (now[t] < 0) sum = __builtin_nanf("");
-            if (g == t) mine = sum;
+            const float was = old;
+            if (step + 64 < stop) ask(step + 64);
+            float mine = 0.f;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int key = step + 16 * t + col;
+                float sum = 0.f;
+#pragma unroll
+                for (int b = 0; b < RB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][t][e], scale, -lse[b][e]));
+                        sum += key < limit[b][e] ? p : 0.f;
+                    }
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                if (__builtin_amdgcn_readlane(ids, (step + 16 * t - window) >> 4) < 0) sum = __builtin_nanf("");
+                if (g == t) mine = sum;
+            }
+            put_weight(a, q, weights, step + lane, mine, was);
         }
-        put_weight(a, q, s, kh, step + lane, mine);
     }
 }
 
@@ -276,7 +280,9 @@ __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, i
     float w = sum[0] + sum[1] + (sum[2] + sum[3]);
     w += __shfl_xor(w, 32);
     if (none) w = __builtin_nanf("");
-    if (h == 0) put_weight(a, q, s, kh, key0 + col, w);
+    if (h != 0) return;
+    const int64_t weights = ((int64_t)s * a.cache.kv_heads + kh) * a.w_stride;
+    put_weight(a, q, weights, key0 + col, w, key0 + col < q.pos0 ? as_global(a.w)[weights + key0 + col] : 0.f);
 }
 
 template <int D, int NW, int CELLS>
@@ -291,13 +297,14 @@ template <int D, int CELLS>
 static void launch_weigh_of(const WeighArgs& a, hipStream_t stream) {
     const int64_t rows = (int64_t)a.seqs.max_q * a.group, units = (int64_t)a.seqs.n_seqs * a.cache.kv_heads;
     const unsigned heads = (unsigned)a.cache.kv_heads, seqs = (unsigned)a.seqs.n_seqs;
-    if (rows <= 32) {
+    // Heads of 256 have no registers for a second block of rows beside the keys.
+    if (rows <= (D == 256 ? 16 : 32)) {
         const int64_t all = (a.seqs.max_kv + 63) / 64;
         const int64_t most = std::max<int64_t>(kMostGroups / heads, 1);             // workgroups of a head
         const int steps = (int)std::max(std::min<int64_t>(std::max<int64_t>(all * units / 2048, 1), 8), (all + 4 * most - 1) / (4 * most));
-        const unsigned blocks = (unsigned)((all + 4 * steps - 1) / (4 * steps));
-        if (rows <= 16) weigh_few_kernel<D, 1, CELLS><<<dim3(blocks * heads, seqs), 256, 0, stream>>>(a, steps);
-        else weigh_few_kernel<D, 2, CELLS><<<dim3(blocks * heads, seqs), 256, 0, stream>>>(a, steps);
+        const dim3 grid((unsigned)((all + 4 * steps - 1) / (4 * steps)) * heads, seqs);
+        if (rows <= 16) weigh_few_kernel<D, 1, CELLS><<<grid, 256, 0, stream>>>(a, steps);
+        else if constexpr (D != 256) weigh_few_kernel<D, 2, CELLS><<<grid, 256, 0, stream>>>(a, steps);
         return;
     }
     constexpr int NW = 4;

@@ -8,7 +8,7 @@ namespace patch {
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }     // as the conversions take it: its exponent field alone
+__device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }     // as the conversions take it: of the exponent's bits alone, whatever the others are
 
 // The values of byte B of w (the low four bits first) times the power, as bf16; all of them are exact there.
 template <int B>
@@ -22,7 +22,7 @@ __device__ __forceinline__ u32x4_t widen8_e2m1(uint32_t w, float power) {
 // Eight bytes, each two features of a key: eight keys of the one feature, and of the other.  p0, p1: the keys' powers.
 struct Two8 { u32x4_t even, odd; };
 __device__ __forceinline__ Two8 turn8_e2m1(uint32_t w0, uint32_t w1, uint32_t p0, uint32_t p1) {
-    const auto power = [](uint32_t p, int b) { return __uint_as_float((b == 0 ? p << 23 : b == 1 ? p << 15 : b == 2 ? p << 7 : p >> 1) & 0x7F800000u); };
+    const auto power = [](uint32_t p, int b) { return __uint_as_float(b == 0 ? p << 23 : b == 1 ? p << 15 : b == 2 ? p << 7 : p >> 1); };    // of bits 23 .. 30 alone
     const uint32_t x[8] = {pair_e2m1<0>(w0, power(p0, 0)), pair_e2m1<1>(w0, power(p0, 1)), pair_e2m1<2>(w0, power(p0, 2)), pair_e2m1<3>(w0, power(p0, 3)),
                            pair_e2m1<0>(w1, power(p1, 0)), pair_e2m1<1>(w1, power(p1, 1)), pair_e2m1<2>(w1, power(p1, 2)), pair_e2m1<3>(w1, power(p1, 3))};
     Two8 t;
