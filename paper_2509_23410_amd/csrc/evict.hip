@@ -67,11 +67,30 @@ struct Ranks {
                 if (j * kStrip + 4 * (int)threadIdx.x + e < length) top = max(top, (int)at[j][e]);
         return top;
     }
-    // what was asked for
-    __device__ __forceinline__ void take(const int32_t* pos, int first, int lowest, int length, const Always& always) {
+    __device__ __forceinline__ void frame(int first, int lowest, int length) {
         base = first;
         begin = lowest;
         len = length;
+    }
+    // J strips full of slots from all over [0, length): every so many fours of them
+    __device__ __forceinline__ void sample(const float* w, const int32_t* pos, int length, const Always& always) {
+        const int64_t fours = length / 4;
+        int i[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            i[j] = 4 * (int)((j * kThreads + (int)threadIdx.x) * fours / (J * kThreads));
+            asked[j] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(w) + i[j]);
+            if (pos) at[j] = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(pos) + i[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[j][e] = rank_of(__uint_as_float(asked[j][e]), always(pos ? (int)at[j][e] : i[j] + e));
+        frame(0, 0, J * kStrip);
+    }
+    // what was asked for
+    __device__ __forceinline__ void take(const int32_t* pos, int first, int lowest, int length, const Always& always) {
+        frame(first, lowest, length);
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -106,12 +125,16 @@ struct Ranks {
 // Histograms are four side by side, of every fourth lane each: an atomic add takes as long as its most frequent address has lanes.
 constexpr int kCopies = 4, kBins = 2048;
 
-template <int J, int RING>
+// Slots whose tokens stay are a bit each where a head has more than registers hold; of so many at most (and ranks near the border in as many pairs of the ring).
+constexpr int kMaskWords = 6656, kNear = 8192;
+
+template <int J, int RING, int MASK>
 struct SelectLds {
     int count[kBins * kCopies];
     uint32_t strip[J][kWaves];         // counts of a strip's wavefronts
     int wave[kWaves], found[3];
     int movers[RING];                  // slots behind the budget whose tokens stay
+    uint32_t mask[MASK];
 };
 
 // front[j] = the sums of x[j] (two counts of 16 bits) over the threads in front of this one in strip j, total[j] = of the whole strip
@@ -148,6 +171,58 @@ __device__ __forceinline__ int sum_of_all(int x, int* wave) {
     return all;
 }
 
+// The `left`-th largest of the ranks that each(f) calls f with, to its first `digits` digits of 11, 11 and 10 bits: the rank (those of them), how many ranks that
+// are the same there are counted with it, and how many of them there are.
+struct Border { uint32_t rank; int left, same; };
+template <typename Lds, typename Each>
+__device__ __forceinline__ Border select(Lds& sh, int digits, int left, const Each& each) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    Border b = {0u, left, 0};
+    for (int digit = 0; digit < digits; ++digit) {
+        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? kBins / 2 : kBins, above = digit == 0 ? 31 : digit == 1 ? 21 : 10;
+        for (int i = tid; i < bins; i += kThreads) *reinterpret_cast<u32x4_t*>(&sh.count[kCopies * i]) = u32x4_t{0, 0, 0, 0};
+        __syncthreads();
+        each([&](uint32_t r) {
+            if (digit == 0 || r >> above == b.rank >> above) atomicAdd(&sh.count[kCopies * ((r >> shift) & (bins - 1)) + (lane & (kCopies - 1))], 1);
+        });
+        __syncthreads();
+        // bins from the largest on, kBins / kThreads a thread (the last digit: half of them): the one in which the sum reaches `left`
+        const auto in_bin = [&](int i) {
+            const u32x4_t n = *reinterpret_cast<const u32x4_t*>(&sh.count[kCopies * i]);
+            return (int)(n[0] + n[1] + n[2] + n[3]);
+        };
+        const int per = bins / kThreads, top = bins - 1 - per * tid;
+        int n[kBins / kThreads], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kBins / kThreads; ++i) {
+            n[i] = i < per ? in_bin(top - i) : 0;
+            sum += n[i];
+        }
+        const int upto = (int)lane_sums((uint32_t)sum);
+        if (lane == 63) sh.wave[tid >> 6] = upto;
+        __syncthreads();
+        int front = upto - sum;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) front += i < tid >> 6 ? sh.wave[i] : 0;
+        if (front < b.left && b.left <= front + sum) {
+#pragma unroll
+            for (int i = 0; i < kBins / kThreads; ++i) {
+                if (front < b.left && b.left <= front + n[i]) {
+                    sh.found[0] = top - i;
+                    sh.found[1] = b.left - front;
+                }
+                front += n[i];
+            }
+        }
+        __syncthreads();
+        b.rank |= (uint32_t)sh.found[0] << shift;
+        b.left = sh.found[1];
+        b.same = in_bin(sh.found[0]);
+        __syncthreads();
+    }
+    return b;
+}
+
 // Slots of a block in their order: which stay, and the ranks of holes and of movers among their like.  `left` of the border's stay, the first ones, `ties` of which have
 // been seen; some: not all of them do.
 template <int J>
@@ -164,8 +239,8 @@ struct Block {
             for (int e = 0; e < 4; ++e) stays[j] |= k.r[j][e] >= border ? 1u << e : 0u;
             stays[j] &= there[j];
         }
-        uint32_t n[J];
         if (some) {
+            uint32_t n[J];
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 n[j] = 0;
@@ -182,6 +257,10 @@ struct Block {
                 *ties += (int)total[j];
             }
         }
+        sums(k, there, strip, keep);
+    }
+    __device__ __forceinline__ void sums(const Ranks<J>& k, const uint32_t (&there)[J], uint32_t (*strip)[kWaves], int keep) {
+        uint32_t n[J];
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int within = min(max(keep - k.slot(j), 0), 4);             // of the thread's four
@@ -232,12 +311,145 @@ struct Block {
     }
 };
 
+// The bits of those that stay, in one pass over the ranks: 16384 of them say between which two the border lies, those above it stay, and only those in between
+// are looked at closely.  A histogram of all takes four times as long, by its atomic adds.  False: the border is not in between, or too many are (or are the same) there.
+template <int J, typename Lds, typename Stream>
+__device__ __forceinline__ bool near_border(Ranks<J>& ranks, Lds& sh, int keep, int len, const float* w, const int32_t* pos, const Always& always, const Stream& stream) {
+    static_assert(J * kStrip == 16384, "a sample");
+    constexpr int kMargin = 320;                                 // five standard deviations of how many of 16384 are above the border, where that is the median
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (len > 32 * kMaskWords) return false;
+    ranks.sample(w, pos, len, always);
+    const int at = (int)((int64_t)keep * (J * kStrip) / len);
+    const auto all = [&](const auto& f) { ranks.each(f); };
+    const uint32_t high = at - kMargin < 1 ? 0xFFFFFFFFu : select(sh, 2, at - kMargin, all).rank | 0x3FFu;
+    const uint32_t low = at + kMargin > J * kStrip ? 0u : select(sh, 2, at + kMargin, all).rank;
+    if (tid == 0) sh.found[2] = 0;
+    __syncthreads();
+    int sure = 0;
+    stream(len, [&] {
+        int mine = 0;
+        uint32_t near[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const uint32_t there = ranks.whole(j) ? 15u : ranks.bits(j);
+            uint32_t stay = 0, maybe = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                stay |= ranks.r[j][e] > high ? 1u << e : 0u;
+                maybe |= ranks.r[j][e] >= low ? 1u << e : 0u;
+            }
+            stay &= there;
+            near[j] = maybe & there & ~stay;
+            sure += __builtin_popcount(stay);
+            mine += __builtin_popcount(near[j]);
+            const uint32_t next = __builtin_amdgcn_update_dpp(0, stay, 0xB1, 0xF, 0xF, true);      // the neighbour's
+            if ((tid & 1) == 0 && ranks.slot(j) < 32 * kMaskWords) reinterpret_cast<uint8_t*>(sh.mask)[ranks.slot(j) >> 3] = (uint8_t)(stay | next << 4);
+        }
+        const int upto = (int)lane_sums((uint32_t)mine);
+        int to = 0;
+        if (lane == 63 && upto) to = atomicAdd(&sh.found[2], upto);
+        to = __builtin_amdgcn_readlane(to, 63) + upto - mine;
+        if (!mine) return;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (near[j] >> e & 1) {
+                    if (to < kNear) {
+                        sh.movers[2 * to] = (int)ranks.r[j][e];
+                        sh.movers[2 * to + 1] = ranks.slot(j) + e;
+                    }
+                    ++to;
+                }
+    });
+    const int need = keep - sum_of_all(sure, sh.wave), n = sh.found[2];
+    if (n > kNear || need < 0 || need > n) return false;
+    if (need == 0) return true;
+    // (their first digits are much the same: what they are above `low` is spread over all bits)
+    const int wide = __builtin_clz((high - low) | 1u);
+    Border border = select(sh, 3, need, [&](const auto& f) {
+        for (int i = tid; i < n; i += kThreads) f(((uint32_t)sh.movers[2 * i] - low) << wide);
+    });
+    border.rank = (border.rank >> wide) + low;
+    const bool some = border.left < border.same;
+    if (some && border.same > kThreads) return false;
+    if (tid == 0) sh.found[2] = 0;
+    __syncthreads();
+    const auto stays = [&](int slot) { atomicOr(&sh.mask[slot >> 5], 1u << (slot & 31)); };
+    for (int i = tid; i < n; i += kThreads) {
+        const uint32_t r = (uint32_t)sh.movers[2 * i];
+        if (r > border.rank || (r == border.rank && !some)) stays(sh.movers[2 * i + 1]);
+        else if (r == border.rank) sh.count[atomicAdd(&sh.found[2], 1)] = sh.movers[2 * i + 1];
+    }
+    __syncthreads();
+    if (some && tid < border.same) {                             // those in the lowest slots
+        const int slot = sh.count[tid];
+        int lower = 0;
+        for (int i = 0; i < border.same; ++i) lower += sh.count[i] < slot;
+        if (lower < border.left) stays(slot);
+    }
+    __syncthreads();
+    return true;
+}
+
+// What is in the slots within the budget, from the bits of those that stay: each thread has words of 32 slots, and the movers of a word's holes follow each other.
+template <typename Lds>
+__device__ __forceinline__ void fill_from_bits(Lds& sh, int keep, int len, int32_t* from) {
+    const int tid = threadIdx.x, lane = tid & 63, words = (len + 31) / 32, per = (words + kThreads - 1) / kThreads, first = min(tid * per, words);
+    int sum = 0;
+    for (int i = first; i < min(first + per, words); ++i) sum += __builtin_popcount(sh.mask[i]);
+    const int upto = (int)lane_sums((uint32_t)sum);
+    if (lane == 63) sh.wave[tid >> 6] = upto;
+    __syncthreads();                                             // (and the list of candidates is done with)
+    int front = upto - sum;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) front += i < tid >> 6 ? sh.wave[i] : 0;
+    int* before = sh.movers;                                     // bits in front of each word
+    for (int i = first; i < min(first + per, words); ++i) {
+        before[i] = front;
+        front += __builtin_popcount(sh.mask[i]);
+    }
+    __syncthreads();
+    const int within = before[keep >> 5] + __builtin_popcount(sh.mask[keep >> 5] & ((1u << (keep & 31)) - 1));       // bits of slots within the budget
+    for (int w = tid; 32 * w < keep; w += kThreads) {
+        const uint32_t stay = sh.mask[w];
+        const int bit = within + 32 * w - before[w];             // that of the first hole's mover
+        int lo = keep >> 5, hi = words - 1;                      // the word that it is in
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (before[mid] <= bit) lo = mid; else hi = mid - 1;
+        }
+        uint32_t rest = sh.mask[lo];
+        for (int i = before[lo]; i < bit; ++i) rest &= rest - 1;
+#pragma unroll 1
+        for (int i = 32 * w; i < min(32 * w + 32, keep); i += 4) {
+            typedef int Four32 __attribute__((ext_vector_type(4), aligned(4)));
+            Four32 came = {i, i + 1, i + 2, i + 3};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (i + e >= keep || (stay >> ((i + e) & 31) & 1)) continue;
+                while (rest == 0 && lo + 1 < words) rest = sh.mask[++lo];
+                came[e] = 32 * lo + __builtin_ctz(rest | 0x80000000u);
+                rest &= rest - 1;
+            }
+            if (i + 3 < keep) {
+                *reinterpret_cast<PATCH_EP_GLOBAL Four32*>(as_global_out(from) + i) = came;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < keep) as_global_out(from)[i + e] = came[e];
+            }
+        }
+    }
+}
+
 // One workgroup for each sequence and key head.  WHOLE: its ranks stay in registers (J strips hold all of them), else they are read again in each pass.
 template <int J, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs a) {
     constexpr int B = WHOLE ? J : 2;                            // strips of a block in the last pass
     constexpr int kRing = WHOLE ? J * kStrip / 2 : 2 * B * kStrip;              // of `len` slots at most half move
-    __shared__ alignas(16) SelectLds<B, kRing> sh;
+    __shared__ alignas(16) SelectLds<B, kRing, WHOLE ? 1 : kMaskWords> sh;
     const int kh = blockIdx.x % a.cache.kv_heads, s = blockIdx.x / a.cache.kv_heads, tid = threadIdx.x, lane = tid & 63, keep = a.keep;
     const int64_t unit = (int64_t)s * a.cache.kv_heads + kh;
     const Seq q = seq_at(a.seqs, s);
@@ -284,109 +496,42 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs 
             f();
         }
     };
-    // the border: `border` is the rank of the last that stays, `left` how many of that rank do, `same` how many have it
-    uint32_t border = 0;
-    int left = keep, same = 0;
-    int candidates = -1;                                         // of the first digit, where the list has room for them: other digits are looked up there
-    for (int digit = 0; digit < 3; ++digit) {
-        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? kBins / 2 : kBins, above = digit == 0 ? 31 : digit == 1 ? 21 : 10;
-        for (int i = tid; i < bins; i += kThreads) *reinterpret_cast<u32x4_t*>(&sh.count[kCopies * i]) = u32x4_t{0, 0, 0, 0};
-        if (!WHOLE && digit == 1 && same <= kRing) {
-            candidates = same;
-            if (tid == 0) sh.found[2] = 0;
-        }
-        __syncthreads();
-        const auto count = [&](uint32_t r) {
-            if (digit == 0 || r >> above == border >> above) atomicAdd(&sh.count[kCopies * ((r >> shift) & (bins - 1)) + (lane & (kCopies - 1))], 1);
-        };
-        if (WHOLE) {
-            ranks.each(count);
-        } else if (candidates < 0) {
-            stream(len, [&] { ranks.each(count); });
-        } else if (digit == 1) {
-            stream(len, [&] {
-                int mine = 0;
-                ranks.each([&](uint32_t r) { mine += r >> above == border >> above; });
-                const int upto = (int)lane_sums((uint32_t)mine);
-                int at = 0;
-                if (lane == 63 && upto) at = atomicAdd(&sh.found[2], upto);
-                at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
-                if (mine)
-                    ranks.each([&](uint32_t r) {
-                        if (r >> above != border >> above) return;
-                        sh.movers[at++] = (int)r;
-                        count(r);
-                    });
-            });
-        } else {
-            for (int i = tid; i < candidates; i += kThreads) count((uint32_t)sh.movers[i]);
-        }
-        __syncthreads();
-        // bins from the largest on, kBins / kThreads a thread (the last digit: half of them): the one in which the sum reaches `left`
-        const auto in_bin = [&](int i) {
-            const u32x4_t n = *reinterpret_cast<const u32x4_t*>(&sh.count[kCopies * i]);
-            return (int)(n[0] + n[1] + n[2] + n[3]);
-        };
-        const int each = bins / kThreads, top = bins - 1 - each * tid;
-        int n[kBins / kThreads], sum = 0;
-#pragma unroll
-        for (int i = 0; i < kBins / kThreads; ++i) {
-            n[i] = i < each ? in_bin(top - i) : 0;
-            sum += n[i];
-        }
-        const int upto = (int)lane_sums((uint32_t)sum);
-        if (lane == 63) sh.wave[tid >> 6] = upto;
-        __syncthreads();
-        int front = upto - sum;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) front += i < tid >> 6 ? sh.wave[i] : 0;
-        if (front < left && left <= front + sum) {
-#pragma unroll
-            for (int i = 0; i < kBins / kThreads; ++i) {
-                if (front < left && left <= front + n[i]) {
-                    sh.found[0] = top - i;
-                    sh.found[1] = left - front;
-                }
-                front += n[i];
-            }
-        }
-        __syncthreads();
-        border |= (uint32_t)sh.found[0] << shift;
-        left = sh.found[1];
-        same = in_bin(sh.found[0]);
-        __syncthreads();
-    }
-
-    const bool some = left < same;                               // not all of the border's stay: those in the lowest slots
     int holes = 0, movers = 0, ties = 0;
     if constexpr (WHOLE) {
+        const Border border = select(sh, 3, keep, [&](const auto& f) { ranks.each(f); });
         Block<J> block;
-        block.look(ranks, sh.strip, keep, border, some, left, &ties);
+        block.look(ranks, sh.strip, keep, border.rank, border.left < border.same, border.left, &ties);
         block.template collect<kRing>(ranks, keep, sh.movers, &movers);
         __syncthreads();
         block.template fill<kRing>(ranks, keep, sh.movers, &holes, from);
     } else {
-        int ties_behind = 0;                                     // the border's behind the budget come after all of those within it
-        if (some) {
-            int mine = 0;
-            stream(keep, [&] { ranks.each([&](uint32_t r) { mine += r == border; }); });
-            ties_behind = sum_of_all(mine, sh.wave);
-        }
-        // as many movers as the holes so far take
         Ranks<B> here, behind;
         Block<B> block, other;
         int ahead = keep & ~3;
+        if (near_border(ranks, sh, keep, len, w, pos, always, stream)) {
+            fill_from_bits(sh, keep, len, from);
+            return;
+        }
+        const Border border = select(sh, 3, keep, [&](const auto& f) { stream(len, [&] { ranks.each(f); }); });
+        const bool some = border.left < border.same;             // not all of the border's stay: those in the lowest slots
+        int ties_behind = 0;                                     // the border's behind the budget come after all of those within it
+        if (some) {
+            int mine = 0;
+            stream(keep, [&] { ranks.each([&](uint32_t r) { mine += r == border.rank; }); });
+            ties_behind = sum_of_all(mine, sh.wave);
+        }
+        // as many movers as the holes so far take
         behind.ask(w, pos, ahead, len);
         here.ask(w, pos, 0, keep);
         for (int first = 0; first < keep; first += B * kStrip) {
             here.take(pos, first, 0, keep, always);
             if (first + B * kStrip < keep) here.ask(w, pos, first + B * kStrip, keep);
-            block.look(here, sh.strip, keep, border, some, left, &ties);
+            block.look(here, sh.strip, keep, border.rank, some, border.left, &ties);
             while (movers < holes + block.holes() && ahead < len) {
                 behind.take(pos, ahead, keep, len, always);
                 ahead += B * kStrip;
                 if (ahead < len) behind.ask(w, pos, ahead, len);
-                other.look(behind, sh.strip, keep, border, some, left, &ties_behind);
+                other.look(behind, sh.strip, keep, border.rank, some, border.left, &ties_behind);
                 other.template collect<kRing>(behind, keep, sh.movers, &movers);
             }
             __syncthreads();

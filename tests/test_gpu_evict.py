@@ -115,6 +115,37 @@ def test_long_ones(cells, kv, keep, recent):
     _check(b, cells, kv, w, stride, keep, 4, recent)
 
 
+@pytest.mark.parametrize("kind", ["plain", "ties", "equal", "odd", "close", "few equal", "runs"])
+def test_long_ones_of_any_weights(kind):
+    """More slots than registers hold: the border between 16384 of the ranks, and where that does not find it (too many are equal, or weights lie in no order that those show)."""
+    kv = [40000, 17000, 300]
+    b = C.batch("e4m3", [1] * 3, kv, 1, 64, 256, seed=3)
+    w, stride = _weights(b, 5, "plain" if kind in ("few equal", "runs") else kind)
+    if kind == "few equal":                                       # 700 of one weight in the middle
+        for s in (0, 1):
+            at = w[s, 0, : kv[s]].sort().indices[kv[s] // 2:kv[s] // 2 + 700]
+            w[s, 0, at] = w[s, 0, at[0]].clone()
+    if kind == "runs":                                            # heavy where the sample of fours does not look, light where it does
+        for s in (0, 1):
+            fours = kv[s] // 4
+            seen = (torch.arange(4096) * fours // 4096 * 4)[:, None] + torch.arange(4)
+            w[s, 0, :] = 1000.0 + torch.arange(stride) % 997
+            w[s, 0, seen.flatten()] = 1.0
+    for keep, sinks, recent in ((8192, 4, 100), (20000, 0, 0), (16999, 0, 500), (1, 0, 0), (39999, 1, 7)):
+        _check(b, "e4m3", kv, w, stride, keep, sinks, recent)
+    g = torch.Generator().manual_seed(2)
+    pos = torch.stack([torch.randperm(stride, generator=g).int() for _ in range(3)]).view(3, 1, stride)
+    _check(b, "e4m3", kv, w, stride, 20000, 4, 3000, pos=pos, in_place=True)
+
+
+def test_longer_than_bits_are_kept_for():
+    b = C.batch("e2m1", [1], [220000], 1, 64, 256, seed=3)
+    w, stride = _weights(b, 5, "plain")
+    _check(b, "e2m1", [220000], w, stride, 90000, 4, 1000)
+    b = C.batch("e2m1", [1], [212992], 1, 64, 256, seed=3)
+    _check(b, "e2m1", [212992], w, stride, 212990, 4, 1000)
+
+
 @pytest.mark.parametrize("cells", CELLS)
 def test_pages_that_are_not_there_and_lengths_that_cannot_be(cells):
     kv = [100, 90, 300, 95]
