@@ -2,8 +2,8 @@
 //
 //   w_j' = decay w_j + sum_r exp(q_r . k_j scale - lse_r)        over a key head's rows r of the call that see key j
 //
-// lse is the attention's own, so a probability needs no pass over the keys before it, and every key's sum is one workgroup's.  The product is S = Q K^T with the
-// rows on the matrix instruction's A side: a column, and so a lane, is a key, and the sum over rows stays in the lane but for its last step.
+// lse is the attention's own, so a probability needs no pass over the keys before it, and every key's sum is one workgroup's: no order but that of the sizes.  The
+// product is S = Q K^T with the rows on the matrix instruction's A side: a column, and so a lane, is a key, and the sum over rows stays in the lane but for its last step.
 #include <algorithm>
 
 #include "attention_kernels.h"
@@ -59,7 +59,9 @@ struct KeyTile {
     }
 };
 
-// Few rows (16 RB at most): each wavefront has `steps` steps of 64 keys, straight from memory into the operands' registers, the next step's on their way.
+// Few rows (16 RB at most): each wavefront has `steps` steps of 64 keys, straight from memory into the operands' registers, the next step's on their way.  Memory
+// bounds it: 32 sequences of up to 8000 tokens, 8 key heads of 128 in 4 bits, 27.6 us, 3.7 TB/s (a large copy: 5.0); with a step's page numbers looked up when it is
+// asked for 38.
 template <int D, int RB, int CELLS>
 __global__ __launch_bounds__(256, 2) void weigh_few_kernel(const WeighArgs a, const int steps) {
     const int s = blockIdx.y, kh = blockIdx.x % a.cache.kv_heads, lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
@@ -145,8 +147,116 @@ __global__ __launch_bounds__(256, 2) void weigh_few_kernel(const WeighArgs a, co
     }
 }
 
+// 32 keys as the second operand of D / 16 products of 32 x 32 x 16, a key a lane; returns whether the lane's has no page.
+template <int D, int CELLS>
+__device__ __forceinline__ bool load_keys(bf16x8_t (&k)[D / 16], const WeighArgs& a, const Seq& q, int s, int kh, int key0) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, key = key0 + (lane & 31);
+    int page = -1;
+    if (key < q.len) page = page_of(a, s, key);
+    const int64_t token = ((int64_t)kh << a.cache.page_log2) + (key & ((1 << a.cache.page_log2) - 1));
+    const PATCH_EP_GLOBAL uint8_t* at = as_global(a.cache.k) + max(page, 0) * a.cache.page_bytes;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        const int64_t cell = token * D + 16 * i + 8 * h;
+        if constexpr (CELLS == kBf16) {
+            k[i] = as_bf16x8(*reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(at + 2 * cell));
+        } else if constexpr (CELLS == kE4m3) {
+            const u32x2_t w = *reinterpret_cast<const PATCH_EP_GLOBAL u32x2_t*>(at + cell);
+            k[i] = as_bf16x8(widen8(w[0], w[1]));
+        } else {
+            const uint32_t w = *reinterpret_cast<const PATCH_EP_GLOBAL uint32_t*>(at + cell / 2);
+            const uint32_t power = as_global(a.cache.k_power)[max(page, 0) * a.cache.power_bytes + cell / 32];
+            k[i] = as_bf16x8(widen8_e2m1(w, power_of(power)));
+        }
+    }
+    return page < 0;
+}
+
+// Many rows and few keys: a workgroup has 32 keys, and its wavefronts take the rows 32 at a time in turn, straight from memory; their sums meet in LDS.
+constexpr int wide_waves(int head_dim) { return head_dim == 256 ? 8 : 16; }       // as many as have registers for it
+
+template <int D, int CELLS>
+__device__ __forceinline__ void weigh_wide(const WeighArgs& a, int s, int kh, int key0) {
+    constexpr int NW = wide_waves(D), kStep = 32 * NW;
+    __shared__ alignas(16) float sh_lse[NW][32], sh_sum[NW][32];
+    __shared__ alignas(16) int sh_limit[NW][32];
+    const Seq q = seq_at(a.seqs, s);
+    if (q.bad || q.n == 0 || key0 >= q.len) return;
+    const int rows = min(q.n, a.seqs.max_q) * a.group, lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const float scale = key_scale(a, CELLS, kh);
+    bf16x8_t k[D / 16];
+    const bool none = load_keys<D, CELLS>(k, a, q, s, kh, key0);
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+    // rows in front see none of the keys; a lane's row follows from the one kStep in front of it
+    const int64_t first = ((int64_t)max(key0 - q.pos0, 0) * a.group & ~(int64_t)31) + 32 * wave;
+    int token = (int)((first + col) / a.group), head = (int)((first + col) % a.group);
+    bf16x8_t query[D / 16];
+    float lse = 0.f;
+    int limit = 0;
+    const auto ask = [&](int r) {
+        const bool there = r + col < rows;
+        const int64_t at = (int64_t)(q.first + (there ? token : 0)) * a.q_stride + (int64_t)(kh * a.group + head) * D + 8 * h;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) query[i] = as_bf16x8(*reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(a.Q) + at + 16 * i));
+        lse = as_global(a.lse)[(int64_t)(q.first + (there ? token : 0)) * a.heads + kh * a.group + head];
+        limit = there ? q.pos0 + token + 1 : 0;
+        head += kStep % a.group;
+        token += kStep / a.group + (head >= a.group);
+        head -= head >= a.group ? a.group : 0;
+    };
+    if (first < rows) ask((int)first);
+    for (int r = (int)first; r < rows; r += kStep) {
+        if (h == 0) {                                            // (of this wavefront's own)
+            sh_lse[wave][col] = lse == kNone ? __builtin_inff() : lse * kLog2e;
+            sh_limit[wave][col] = limit;
+        }
+        const bool ragged = r + 32 > rows || key0 + 32 > __builtin_amdgcn_readfirstlane(limit);
+        f32x16_t x;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(query[i], k[i], x, 0, 0, 0);
+        if (r + kStep < rows) ask(r + kStep);
+        const auto add = [&](auto masked) {
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const f32x4_t l = *reinterpret_cast<const f32x4_t*>(&sh_lse[wave][8 * e4 + 4 * h]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * e4 + e], scale, -l[e]));
+                    if constexpr (decltype(masked)::value) p = key0 + col < sh_limit[wave][8 * e4 + 4 * h + e] ? p : 0.f;
+                    sum[e] += p;
+                }
+            }
+        };
+        if (ragged) add(std::true_type{});
+        else add(std::false_type{});
+    }
+    float w = sum[0] + sum[1] + (sum[2] + sum[3]);
+    w += __shfl_xor(w, 32);
+    if (h == 0) sh_sum[wave][col] = w;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        w = 0.f;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) w += sh_sum[i][col];
+        if (none) w = __builtin_nanf("");
+        const int64_t weights = ((int64_t)s * a.cache.kv_heads + kh) * a.w_stride;
+        put_weight(a, q, weights, key0 + col, w, key0 + col < q.pos0 ? as_global(a.w)[weights + key0 + col] : 0.f);
+    }
+    __syncthreads();
+}
+
+template <int D, int CELLS>
+__global__ __launch_bounds__(64 * wide_waves(D)) void weigh_wide_kernel(const WeighArgs a) {
+    for (int64_t key = blockIdx.x / a.cache.kv_heads * 32; key < a.seqs.max_kv; key += gridDim.x / a.cache.kv_heads * 32)
+        weigh_wide<D, CELLS>(a, blockIdx.y, blockIdx.x % a.cache.kv_heads, (int)key);
+}
+
 // Many rows: a workgroup's wavefronts have 32 keys each, in registers as operands, and the rows come through LDS for all of them, 64 at a time, the next ones
-// on their way through registers meanwhile.
+// on their way through registers meanwhile.  A prompt of 4096, 32 heads of 128: 102 us, 675 TFLOP/s; without its loads 84, without exp2 95, with a quarter of
+// its products 75: no one of them bounds it, but the wait of all wavefronts for each other at each 64 rows.
 template <int D>
 struct RowTilesLds {
     u32x4_t q[2][64 * D / 8];
@@ -161,32 +271,10 @@ __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, i
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Seq q = seq_at(a.seqs, s);
     if (q.bad || q.n == 0 || block >= q.len) return;
-    const int rows = min(q.n, a.seqs.max_q) * a.group, key0 = block + wave * kKeys, mask = (1 << a.cache.page_log2) - 1;
+    const int rows = min(q.n, a.seqs.max_q) * a.group, key0 = block + wave * kKeys;
     const float scale = key_scale(a, CELLS, kh);
     bf16x8_t k[D / 16];
-    bool none;
-    {
-        const int key = key0 + col;
-        int page = -1;
-        if (key < q.len) page = page_of(a, s, key);
-        none = page < 0;
-        const int64_t token = ((int64_t)kh << a.cache.page_log2) + (key & mask);
-        const PATCH_EP_GLOBAL uint8_t* at = as_global(a.cache.k) + max(page, 0) * a.cache.page_bytes;
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-            const int64_t cell = token * D + 16 * i + 8 * h;
-            if constexpr (CELLS == kBf16) {
-                k[i] = as_bf16x8(*reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(at + 2 * cell));
-            } else if constexpr (CELLS == kE4m3) {
-                const u32x2_t w = *reinterpret_cast<const PATCH_EP_GLOBAL u32x2_t*>(at + cell);
-                k[i] = as_bf16x8(widen8(w[0], w[1]));
-            } else {
-                const uint32_t w = *reinterpret_cast<const PATCH_EP_GLOBAL uint32_t*>(at + cell / 2);
-                const uint32_t power = as_global(a.cache.k_power)[max(page, 0) * a.cache.power_bytes + cell / 32];
-                k[i] = as_bf16x8(widen8_e2m1(w, power_of(power)));
-            }
-        }
-    }
+    const bool none = load_keys<D, CELLS>(k, a, q, s, kh, key0);
     f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 
     const int row = tid / kRowLoads, chunk = tid % kRowLoads;
@@ -307,9 +395,16 @@ static void launch_weigh_of(const WeighArgs& a, hipStream_t stream) {
         else if constexpr (D != 256) weigh_few_kernel<D, 2, CELLS><<<grid, 256, 0, stream>>>(a, steps);
         return;
     }
+    const auto blocks = [&](int keys) { return (unsigned)std::min<int64_t>((a.seqs.max_kv + keys - 1) / keys, std::max<int64_t>(kMostGroups / heads, 1)) * heads; };
     constexpr int NW = 4;
-    const int64_t blocks = std::min<int64_t>((a.seqs.max_kv + 32 * NW - 1) / (32 * NW), std::max<int64_t>(kMostGroups / heads, 1));
-    weigh_tiles_kernel<D, NW, CELLS><<<dim3((unsigned)blocks * heads, seqs), 64 * NW, 0, stream>>>(a);
+    // Where blocks of 128 keys do not fill the chip, or leave it to the first keys' (which all rows see) for half of the time: one prompt of 2048 tokens, 16 query heads
+    // over 1 of 128, 621 us so and 230 with the rows dealt to wavefronts, 32 over 8 160 and 74; of 4096 tokens, 32 over 8 (256 blocks, 16384 rows), 318 and 261, but
+    // of 1000 tokens, 32 over 32 (256 blocks, 1000 rows), 23.5 and 38.
+    const int64_t groups = (int64_t)blocks(32 * NW) * seqs;
+    if (groups < 128 || (groups <= 256 && rows >= 4096))
+        weigh_wide_kernel<D, CELLS><<<dim3(blocks(32), seqs), 64 * wide_waves(D), 0, stream>>>(a);
+    else
+        weigh_tiles_kernel<D, NW, CELLS><<<dim3(blocks(32 * NW), seqs), 64 * NW, 0, stream>>>(a);
 }
 template <int CELLS>
 static void launch_weigh_cells(const WeighArgs& a, hipStream_t stream) {
