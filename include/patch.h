@@ -559,7 +559,8 @@ typedef struct {
 
 /* patch_kv_append into 4-bit cells.  The power of 32 values is the smallest of which the largest magnitude is at most seven, from 2^-100 to
  * 2^125; a cell is the value over the power rounded to the nearest, ties to even codes, and six where it is beyond six.  32 values one
- * of which is a NaN or infinite become NaN.
+ * of which is a NaN or infinite become NaN.  Where two tokens of a batch have the same place, what is there is of neither (codes of the
+ * one may meet powers of the other).
  *   k->out, v->out  bf16 rows for what the new tokens' cells stand for (exact in bf16), or NULL; rows without a place become zeros
  *   positions       DEVICE, n_tokens: where the rotation takes a token to be, for caches that tokens were evicted from; one outside
  *                   0 .. n_pos - 1 turns by NaN.  NULL: its position in the cache.
@@ -608,7 +609,7 @@ typedef struct {
  * `keep` that stay do so where they are; the others, in the order of their slots, move into the slots there that became free, in
  * theirs.  So keys are in no order afterwards and differ from head to head: new tokens are appended behind them as always, with
  * positions given for their rotation.
- *   seqs   n_seqs, kv_len, page_table, table_stride and max_kv; n_tokens, q_start and max_q are not looked at
+ *   seqs   n_seqs (times kv_heads at most 2^21), kv_len, page_table, table_stride and max_kv; n_tokens, q_start and max_q are not looked at
  *   W      DEVICE, n_seqs x kv_heads rows of `stride` >= max_kv floats, 16-byte aligned, stride a multiple of 4
  * Pages that two sequences share may only be in front of their sinks.  Cells whose page, or whose goal's, is not followed stay; a
  * sequence longer than max_kv or the table stays as it is (`from` is -1).  Errors: PATCH_ERR_ARG, PATCH_ERR_SHAPE, PATCH_ERR_HIP. */

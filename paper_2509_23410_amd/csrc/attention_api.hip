@@ -289,7 +289,7 @@ static patch_status evict(const patch_seqs* seqs, const Cache* cache, const floa
     only.max_q = 0;
     TRY(fill_seqs(&a.seqs, &only, cache->page_size));
     if (stride < a.seqs.max_kv || stride > ((int64_t)1 << 32) || stride % 4) return PATCH_ERR_SHAPE;
-    if (seqs->n_seqs * cache->kv_heads > (1 << 22)) return PATCH_ERR_SHAPE;
+    if (seqs->n_seqs * cache->kv_heads > (1 << 21)) return PATCH_ERR_SHAPE;    // workgroups of 1024 threads
     a.w = W;
     a.w_out = opts->W_out;
     a.w_stride = stride;

@@ -326,7 +326,7 @@ __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, i
         ask(first);
         put(0);
     }
-    // the keys are there: else the first product of each step waits for them, and with them for the rows that were asked for since (125 us for 82)
+    // the keys are there before the loop: else the first products of each step wait for them, and so for the rows that were asked for since
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();
     int buffer = 0;

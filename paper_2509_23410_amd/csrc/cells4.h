@@ -1,6 +1,9 @@
 // Cells of 4 bits: e2m1 (0 .5 1 1.5 2 3 4 6 and a sign), two to a byte, times a power of two that 32 features of a token share: a byte, 2^(byte - 127), 255
-// for a NaN.  The power is the smallest of which the largest of the 32 is at most seven: a value that would be nearer to 8 than to 6 powers is then the only one
-// that is off by more than half of a step, and there is none.
+// for a NaN.  The power is the smallest of which the largest of the 32 is at most seven: up to there six is off by no more than one power, which is half of the step
+// between four and six; with the smallest of which it is at most six the other values would have steps twice as wide for those between.
+//
+// gfx950 converts a byte's two cells, with the power, in one instruction.  A byte of V is two features of one token, so that both have one power, and no token
+// shares a byte with another: one by itself is appended, or moved, by stores of whole bytes.
 #pragma once
 #include "cells.h"
 

@@ -97,7 +97,7 @@ EVICTS = [("call", dict(W=None), B.ERR_ARG), ("call", dict(W=P + 4), B.ERR_ARG),
           ("call", dict(keep=0), B.ERR_ARG), ("call", dict(keep=-1), B.ERR_ARG), ("call", dict(keep=(1 << 29) + 1), B.ERR_ARG), ("call", dict(sinks=-1), B.ERR_ARG),
           ("call", dict(recent=-1), B.ERR_ARG), ("call", dict(sinks=33, recent=32), B.ERR_ARG), ("call", dict(sinks=65), B.ERR_ARG), ("call", dict(recent=1 << 62, sinks=1), B.ERR_ARG),
           ("call", dict(moved_from=None), B.ERR_ARG), ("call", dict(moved_from=P + 2), B.ERR_ARG), ("call", dict(kv_len_out=None), B.ERR_ARG), ("call", dict(kv_len_out=P + 1), B.ERR_ARG),
-          ("call", dict(positions=P + 4), B.ERR_ARG), ("call", dict(positions_out=P + 4), B.ERR_ARG), ("seqs", dict(n_seqs=65535), B.ERR_SHAPE)]
+          ("call", dict(positions=P + 4), B.ERR_ARG), ("call", dict(positions_out=P + 4), B.ERR_ARG), ("seqs", dict(n_seqs=65535), B.ERR_SHAPE), ("seqs", dict(n_seqs=16385), B.ERR_SHAPE)]
 
 
 @pytest.mark.parametrize("four", [False, True])
@@ -105,7 +105,7 @@ EVICTS = [("call", dict(W=None), B.ERR_ARG), ("call", dict(W=P + 4), B.ERR_ARG),
 def test_evict_refuses(which, kw, want, four):
     a = dict(dict(W=P, W_out=P, stride=128, keep=64, moved_from=P, kv_len_out=P), **(kw if which == "call" else {}))
     args = [a.pop(x) for x in ("W", "W_out", "stride", "keep", "moved_from", "kv_len_out")]
-    wide = dict(kv_heads=128) if kw == dict(n_seqs=65535) else {}
+    wide = dict(kv_heads=128) if "n_seqs" in kw and kw["n_seqs"] in (65535, 16385) else {}
     call, c = (B.patch_kv_evict4, cache4(**wide)) if four else (B.patch_kv_evict, cache(**wide))
     assert status(call, seqs(**(kw if which == "seqs" else {})), c, *args, **a) == want
 

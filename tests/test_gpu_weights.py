@@ -44,7 +44,9 @@ CASES = [
     ([1, 0, 1], [700, 50, 2100], 4, 2, 256, 128), ([1] * 9, [600, 601, 640, 700, 513, 514, 900, 1, 0], 40, 2, 128, 64), ([5] * 3, [300, 310, 205], 10, 2, 128, 16),
     ([4, 0, 7, 1], [40, 17, 300, 60], 16, 1, 128, 32), ([3, 2], [300, 299], 14, 2, 64, 256), ([8, 3], [3, 3], 4, 2, 128, 16), ([33, 1, 20], [33, 90, 100], 8, 2, 64, 16),
     ([130], [130], 2, 1, 128, 64), ([90, 150, 7], [200, 150, 500], 4, 1, 256, 64), ([270, 40], [600, 333], 3, 3, 128, 32), ([257], [1300], 2, 2, 256, 256),
-    ([64, 300], [64, 20], 6, 2, 64, 16)]
+    ([64, 300], [64, 20], 6, 2, 64, 16),
+    # enough blocks of keys for rows through LDS
+    ([40, 33, 70, 65] * 9, [40, 100, 200, 65] * 9, 8, 4, 64, 16), ([40, 0, 70, 129] * 9, [140, 100, 200, 65] * 9, 12, 4, 128, 64), ([33, 20] * 20, [330, 60] * 20, 4, 4, 256, 32)]
 
 
 @pytest.mark.parametrize("cells", ["bf16", "e4m3", "e2m1"])
