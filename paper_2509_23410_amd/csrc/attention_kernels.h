@@ -809,6 +809,21 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+            if constexpr (CELLS == kE2m1) {
+                // the same by hand: here the compiler does not follow the order below by itself
+                constexpr int kProducts = kBlocks * D / 16, kLead = 6;
+                const auto operand = [&](int j) { return as_bf16x8(sh.k[buffer][chunk_at<D / 8>(32 * (j % kBlocks) + col, 2 * (j / kBlocks) + h)]); };
+                bf16x8_t ahead[kLead];
+#pragma unroll
+                for (int j = 0; j < kLead && j < kProducts; ++j) ahead[j] = operand(j);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < kProducts; ++j) {
+                    s[j % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[j % kLead], q[j / kBlocks], s[j % kBlocks], 0, 0, 0);
+                    if (j + kLead < kProducts) ahead[j % kLead] = operand(j + kLead);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -822,6 +837,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
                 __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
             __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
+            }
             __builtin_amdgcn_s_setprio(0);
             const bool ragged = tile < p.key0 || tile + kTile > fewest;
             if (ragged) {
