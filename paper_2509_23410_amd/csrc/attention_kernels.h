@@ -609,8 +609,8 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const Span& p, in
 }
 
 // Many rows: a workgroup's wavefronts have 32 rows each, and the keys come through LDS for all of them, kTile at a time, the next ones on their way through
-// registers meanwhile.  The products are the ones above on 32 x 32 x 16 instructions.  A prompt of 4096 over 32 heads of 128: 167 - 178 us on different cards,
-// 825 - 770 TFLOP/s; with operands from registers alone it would be 116, with the reads from LDS (all of K and V for each wavefront) and no softmax 160: those
+// registers meanwhile.  The products are the ones above on 32 x 32 x 16 instructions.  A prompt of 4096 over 32 heads of 128: 155 - 163 us on different cards,
+// 885 - 845 TFLOP/s; with operands from registers alone it would be 116, with the reads from LDS (all of K and V for each wavefront) and no softmax 160: those
 // two bound it.  27 % of the LDS' busy cycles are bank conflicts; which of its reads and writes have them has not been found out.
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
@@ -631,6 +631,25 @@ struct TilesLds {
     int infinite[2][NW], fewest[NW], pages[kTableKeys / 16];
     float m[32 * NW];
 };
+
+// product(j, operand(j)) for j = 0 .. N - 1, in this order and with five operands asked for ahead: left to itself the compiler asks for one at a time, and waits.
+// Both products of the tiles so, against the order asked for with sched_group_barrier in the first and none in the second: 6 pieces of up to 700 tokens over
+// 8 key heads of 4 151 us before and 138 so in bf16, 165 and 141 in e4m3, 167 and 146 in e2m1; a prompt of 4096 over 32 heads of 128 in bf16 165 and 156.
+// Six ahead take the same time but spill at 128 features.
+template <int N, typename Operand, typename Product>
+__device__ __forceinline__ void in_order(const Operand& operand, const Product& product) {
+    constexpr int kLead = N < 5 ? N : 5;
+    bf16x8_t ahead[kLead];
+#pragma unroll
+    for (int j = 0; j < kLead; ++j) ahead[j] = operand(j);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        product(j, ahead[j % kLead]);
+        if (j + kLead < N) ahead[j % kLead] = operand(j + kLead);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
 
 // 32 NW rows of a span from first_row on, by a workgroup of NW wavefronts.
 template <int D, int NW, int CELLS>
@@ -809,35 +828,9 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
-            if constexpr (CELLS == kE2m1) {
-                // the same by hand: here the compiler does not follow the order below by itself
-                constexpr int kProducts = kBlocks * D / 16, kLead = 6;
-                const auto operand = [&](int j) { return as_bf16x8(sh.k[buffer][chunk_at<D / 8>(32 * (j % kBlocks) + col, 2 * (j / kBlocks) + h)]); };
-                bf16x8_t ahead[kLead];
-#pragma unroll
-                for (int j = 0; j < kLead && j < kProducts; ++j) ahead[j] = operand(j);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int j = 0; j < kProducts; ++j) {
-                    s[j % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[j % kLead], q[j / kBlocks], s[j % kBlocks], 0, 0, 0);
-                    if (j + kLead < kProducts) ahead[j % kLead] = operand(j + kLead);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            } else {
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
-                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh.k[buffer][chunk_at<D / 8>(32 * b + col, 2 * i + h)]), q[i], s[b], 0, 0, 0);
             // the operands of the next few products are on their way out of LDS while one runs
-            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-            for (int i = 0; i < kBlocks * D / 16 - 6; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
-            }
+            in_order<kBlocks * D / 16>([&](int j) { return as_bf16x8(sh.k[buffer][chunk_at<D / 8>(32 * (j % kBlocks) + col, 2 * (j / kBlocks) + h)]); },
+                                       [&](int j, bf16x8_t k) { s[j % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[j / kBlocks], s[j % kBlocks], 0, 0, 0); });
             __builtin_amdgcn_s_setprio(0);
             const bool ragged = tile < p.key0 || tile + kTile > fewest;
             if (ragged) {
@@ -879,11 +872,10 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, i
 #pragma unroll
                 for (int w = 0; w < NW; ++w) redo |= sh.infinite[buffer][w] != 0;
             }
-#pragma unroll
-            for (int k = 0; k < kTile / 16; ++k)
-#pragma unroll
-                for (int i = 0; i < DV / 32; ++i)
-                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh.v[buffer][chunk_at<kTile / 8>(32 * i + col, 2 * k + h)]), pr[k], o[i], 0, 0, 0);
+            in_order<kTile / 16 * (DV / 32)>([&](int j) { return as_bf16x8(sh.v[buffer][chunk_at<kTile / 8>(32 * (j % (DV / 32)) + col, 2 * (j / (DV / 32)) + h)]); },
+                                             [&](int j, bf16x8_t v) {
+                                                 o[j % (DV / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pr[j / (DV / 32)], o[j % (DV / 32)], 0, 0, 0);
+                                             });
         }
         if (more) put_keys(tile + kTile, buffer ^ 1);
         __syncthreads();
