@@ -255,8 +255,9 @@ __global__ __launch_bounds__(64 * wide_waves(D)) void weigh_wide_kernel(const We
 }
 
 // Many rows: a workgroup's wavefronts have 32 keys each, in registers as operands, and the rows come through LDS for all of them, 64 at a time, the next ones
-// on their way through registers meanwhile.  A prompt of 4096, 32 heads of 128: 102 us, 675 TFLOP/s; without its loads 84, without exp2 95, with a quarter of
-// its products 75: no one of them bounds it, but the wait of all wavefronts for each other at each 64 rows.
+// on their way through registers meanwhile.  A prompt of 4096, 32 heads of 128: 96 us, 715 TFLOP/s; 101 with the products of 32 rows after those of the other 32 and
+// operands left to the compiler.  Of those 101, 84 without its loads, 95 without exp2, 75 with a quarter of its products: no one of them bounds it, but the wait of
+// all wavefronts for each other at each 64 rows.
 template <int D>
 struct RowTilesLds {
     u32x4_t q[2][64 * D / 8];
@@ -337,14 +338,16 @@ __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, i
         const int lowest = __builtin_amdgcn_readfirstlane(sh.limit[buffer][0]), highest = __builtin_amdgcn_readfirstlane(sh.limit[buffer][min(rows - tile, 64) - 1]);
         if (key0 < highest) {
             const bool ragged = tile + 64 > rows || key0 + kKeys > lowest;       // not every row is there and sees all of the keys
+            f32x16_t both[2];
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) both[half][e] = 0.f;
+            in_order<D / 8>([&](int j) { return as_bf16x8(sh.q[buffer][chunk_at<D / 8>(32 * (j % 2) + col, 2 * (j / 2) + h)]); },
+                            [&](int j, bf16x8_t row) { both[j % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row, k[j / 2], both[j % 2], 0, 0, 0); });
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                f32x16_t x;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = 0.f;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-                    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(sh.q[buffer][chunk_at<D / 8>(32 * half + col, 2 * i + h)]), k[i], x, 0, 0, 0);
+                const f32x16_t& x = both[half];
                 const auto add = [&](auto masked) {
 #pragma unroll
                     for (int e4 = 0; e4 < 4; ++e4) {
