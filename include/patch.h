@@ -586,7 +586,7 @@ typedef struct {
  * before it (W is not read there).  For sequences with tokens in the call and j < kv_len[s]; everything else stays as it is.
  *   Q, q_stride, heads  as in patch_attention, whose lse (n_tokens x heads) for these rows is `lse`
  *   W, W_out            DEVICE, n_seqs x kv_heads rows of `stride` >= max_kv floats, 16-byte aligned, stride a multiple of 4; W_out may be W
- * A row whose lse is minus infinity (it saw nothing) adds nothing.  Sums are fp32, in an order that the sizes alone decide.  Pages that are
+ * A row whose lse is minus infinity (it saw nothing) adds nothing, whatever its query and the keys are.  Sums are fp32, in an order that the sizes alone decide.  Pages that are
  * not followed have NaN for keys.  Errors: PATCH_ERR_ARG, PATCH_ERR_SHAPE, PATCH_ERR_HIP. */
 patch_status patch_attention_weights(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const float* lse,
                                      const float* W, float* W_out, int64_t stride, void* stream, const patch_weights_opts* opts);

@@ -4,6 +4,8 @@
 //
 // lse is the attention's own, so a probability needs no pass over the keys before it, and every key's sum is one workgroup's: no order but that of the sizes.  The
 // product is S = Q K^T with the rows on the matrix instruction's A side: a column, and so a lane, is a key, and the sum over rows stays in the lane but for its last step.
+//
+// A row whose lse is minus infinity is as one that is not there: it sees no key (its limit is 0), since its scores may be NaN, which no lse makes nothing of.
 #include <algorithm>
 
 #include "attention_kernels.h"
@@ -13,12 +15,6 @@ namespace patch {
 constexpr int64_t kMostGroups = (int64_t)1 << 22;             // workgroups in x: far from the 2^32 threads that one launch may have there
 constexpr float kLog2e = 1.4426950408889634f;
 
-// lse of row r of a sequence's head times log2(e), plus infinity where there is nothing to add
-__device__ __forceinline__ float lse_of(const WeighArgs& a, int first, int rows, int kh, int r) {
-    if (r >= rows) return __builtin_inff();
-    const float l = as_global(a.lse)[(int64_t)(first + r / a.group) * a.heads + kh * a.group + r % a.group] * kLog2e;
-    return l == kNone ? __builtin_inff() : l;
-}
 // what is written for key j of a sequence, whose head's weights begin at `weights`: `sum` is of the call's rows, `old` what was there for a key that is not new
 __device__ __forceinline__ void put_weight(const WeighArgs& a, const Seq& q, int64_t weights, int j, float sum, float old) {
     if (j >= q.len) return;
@@ -84,11 +80,17 @@ __global__ __launch_bounds__(256, 2) void weigh_few_kernel(const WeighArgs a, co
             if (r < rows) v = *reinterpret_cast<const PATCH_EP_GLOBAL u32x4_t*>(as_global(a.Q) + at + query_offset<D, CELLS>(i, g));
             query[b][i] = as_bf16x8(v);
         }
+        int token = (16 * b + 4 * g) / a.group, head = (16 * b + 4 * g) % a.group;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int row = 16 * b + 4 * g + e;
-            lse[b][e] = lse_of(a, q.first, rows, kh, row);
-            limit[b][e] = row < rows ? q.pos0 + row / a.group + 1 : 0;
+        for (int e = 0; e < 4; ++e) {                            // no branch: all of them on their way together
+            const bool there = 16 * b + 4 * g + e < rows;
+            const float l = as_global(a.lse)[(int64_t)(q.first + (there ? token : 0)) * a.heads + kh * a.group + head];
+            lse[b][e] = l * kLog2e;
+            limit[b][e] = there && l != kNone ? q.pos0 + token + 1 : 0;
+            if (++head == a.group) {
+                head = 0;
+                ++token;
+            }
         }
     }
     typedef KeyTile<D, CELLS> Tile;
@@ -130,16 +132,16 @@ __global__ __launch_bounds__(256, 2) void weigh_few_kernel(const WeighArgs a, co
             for (int t = 0; t < 4; ++t) {
                 const int key = step + 16 * t + col;
                 float sum = 0.f;
+                const float by = __builtin_amdgcn_readlane(ids, (step + 16 * t - window) >> 4) < 0 ? __builtin_nanf("") : scale;       // no page: NaN for whichever row sees the key
 #pragma unroll
                 for (int b = 0; b < RB; ++b)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][t][e], scale, -lse[b][e]));
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][t][e], by, -lse[b][e]));
                         sum += key < limit[b][e] ? p : 0.f;
                     }
                 sum += __shfl_xor(sum, 16);
                 sum += __shfl_xor(sum, 32);
-                if (__builtin_amdgcn_readlane(ids, (step + 16 * t - window) >> 4) < 0) sum = __builtin_nanf("");
                 if (g == t) mine = sum;
             }
             put_weight(a, q, weights, step + lane, mine, was);
@@ -147,7 +149,7 @@ __global__ __launch_bounds__(256, 2) void weigh_few_kernel(const WeighArgs a, co
     }
 }
 
-// 32 keys as the second operand of D / 16 products of 32 x 32 x 16, a key a lane; returns whether the lane's has no page.
+// 32 keys as the second operand of D / 16 products of 32 x 32 x 16, a key a lane; returns whether the lane's has a page.
 template <int D, int CELLS>
 __device__ __forceinline__ bool load_keys(bf16x8_t (&k)[D / 16], const WeighArgs& a, const Seq& q, int s, int kh, int key0) {
     const int lane = threadIdx.x & 63, h = lane >> 5, key = key0 + (lane & 31);
@@ -169,7 +171,7 @@ __device__ __forceinline__ bool load_keys(bf16x8_t (&k)[D / 16], const WeighArgs
             k[i] = as_bf16x8(widen8_e2m1(w, power_of(power)));
         }
     }
-    return page < 0;
+    return page >= 0;
 }
 
 // Many rows and few keys: a workgroup has 32 keys, and its wavefronts take the rows 32 at a time in turn, straight from memory; their sums meet in LDS.
@@ -184,9 +186,9 @@ __device__ __forceinline__ void weigh_wide(const WeighArgs& a, int s, int kh, in
     if (q.bad || q.n == 0 || key0 >= q.len) return;
     const int rows = min(q.n, a.seqs.max_q) * a.group, lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const float scale = key_scale(a, CELLS, kh);
     bf16x8_t k[D / 16];
-    const bool none = load_keys<D, CELLS>(k, a, q, s, kh, key0);
+    float scale = key_scale(a, CELLS, kh);
+    if (!load_keys<D, CELLS>(k, a, q, s, kh, key0)) scale = __builtin_nanf("");       // for whichever row sees the key
     f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
     // rows in front see none of the keys; a lane's row follows from the one kStep in front of it
     const int64_t first = ((int64_t)max(key0 - q.pos0, 0) * a.group & ~(int64_t)31) + 32 * wave;
@@ -207,11 +209,12 @@ __device__ __forceinline__ void weigh_wide(const WeighArgs& a, int s, int kh, in
     };
     if (first < rows) ask((int)first);
     for (int r = (int)first; r < rows; r += kStep) {
+        const int sees = lse == kNone ? 0 : limit;               // 0 also for rows that are not there
         if (h == 0) {                                            // (of this wavefront's own)
-            sh_lse[wave][col] = lse == kNone ? __builtin_inff() : lse * kLog2e;
-            sh_limit[wave][col] = limit;
+            sh_lse[wave][col] = lse * kLog2e;
+            sh_limit[wave][col] = sees;
         }
-        const bool ragged = r + 32 > rows || key0 + 32 > __builtin_amdgcn_readfirstlane(limit);
+        const bool ragged = __any(key0 + 32 > sees);
         f32x16_t x;
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = 0.f;
@@ -241,7 +244,6 @@ __device__ __forceinline__ void weigh_wide(const WeighArgs& a, int s, int kh, in
         w = 0.f;
 #pragma unroll
         for (int i = 0; i < NW; ++i) w += sh_sum[i][col];
-        if (none) w = __builtin_nanf("");
         const int64_t weights = ((int64_t)s * a.cache.kv_heads + kh) * a.w_stride;
         put_weight(a, q, weights, key0 + col, w, key0 + col < q.pos0 ? as_global(a.w)[weights + key0 + col] : 0.f);
     }
@@ -262,7 +264,7 @@ template <int D>
 struct RowTilesLds {
     u32x4_t q[2][64 * D / 8];
     float lse[2][64];
-    int limit[2][64];
+    int limit[2][64], out[2];             // the first key that a row does not see, 0 for one that adds nothing or is not there; whether there are such
 };
 
 template <int D, int NW, int CELLS>
@@ -273,9 +275,9 @@ __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, i
     const Seq q = seq_at(a.seqs, s);
     if (q.bad || q.n == 0 || block >= q.len) return;
     const int rows = min(q.n, a.seqs.max_q) * a.group, key0 = block + wave * kKeys;
-    const float scale = key_scale(a, CELLS, kh);
     bf16x8_t k[D / 16];
-    const bool none = load_keys<D, CELLS>(k, a, q, s, kh, key0);
+    float scale = key_scale(a, CELLS, kh);
+    if (!load_keys<D, CELLS>(k, a, q, s, kh, key0)) scale = __builtin_nanf("");       // for whichever row sees the key
     f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 
     const int row = tid / kRowLoads, chunk = tid % kRowLoads;
@@ -295,6 +297,10 @@ __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, i
     const PATCH_EP_GLOBAL uint16_t* queries = as_global(a.Q) + (int64_t)q.first * a.q_stride + (int64_t)kh * a.group * D + 8 * chunk;
     // the first wavefront has their lse, too
     int lse_token = (first + lane) / a.group, lse_head = (first + lane) % a.group;
+    // tokens of a tile's first row and of its 64th
+    int low = __builtin_amdgcn_readlane(lse_token, 0), low_head = __builtin_amdgcn_readlane(lse_head, 0);
+    int high = __builtin_amdgcn_readlane(lse_token, 63), high_head = __builtin_amdgcn_readlane(lse_head, 63);
+    const int last = min(q.n, a.seqs.max_q) - 1;
     u32x4_t regs[kEach];
     float lse_reg = 0.f;
     int limit_reg = 0;
@@ -319,8 +325,9 @@ __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, i
 #pragma unroll
         for (int i = 0; i < kEach; ++i) sh.q[buffer][chunk_at<D / 8>(row + i * kRowStep, chunk)] = regs[i];
         if (wave == 0) {
-            sh.lse[buffer][lane] = lse_reg == kNone ? __builtin_inff() : lse_reg * kLog2e;
-            sh.limit[buffer][lane] = limit_reg;
+            sh.lse[buffer][lane] = lse_reg * kLog2e;
+            sh.limit[buffer][lane] = lse_reg == kNone ? 0 : limit_reg;
+            sh.out[buffer] = __any(lse_reg == kNone || limit_reg == 0);
         }
     };
     if (first < rows) {
@@ -331,13 +338,19 @@ __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, i
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();
     int buffer = 0;
+    const auto forward = [&](int& token, int& head) {
+        head += heads64;
+        token += 64 / a.group + (head >= a.group);
+        head -= head >= a.group ? a.group : 0;
+    };
     for (int tile = first; tile < rows; tile += 64, buffer ^= 1) {
         const bool more = tile + 64 < rows;
+        const int lowest = q.pos0 + low + 1, highest = q.pos0 + min(high, last) + 1;       // limits never fall from row to row, but for rows that are out
+        forward(low, low_head);
+        forward(high, high_head);
         if (more) ask(tile + 64);
-        // limits never fall from row to row, and those of no rows are 0
-        const int lowest = __builtin_amdgcn_readfirstlane(sh.limit[buffer][0]), highest = __builtin_amdgcn_readfirstlane(sh.limit[buffer][min(rows - tile, 64) - 1]);
         if (key0 < highest) {
-            const bool ragged = tile + 64 > rows || key0 + kKeys > lowest;       // not every row is there and sees all of the keys
+            const int out = sh.out[buffer];
             f32x16_t both[2];
 #pragma unroll
             for (int half = 0; half < 2; ++half)
@@ -345,6 +358,7 @@ __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, i
                 for (int e = 0; e < 16; ++e) both[half][e] = 0.f;
             in_order<D / 8>([&](int j) { return as_bf16x8(sh.q[buffer][chunk_at<D / 8>(32 * (j % 2) + col, 2 * (j / 2) + h)]); },
                             [&](int j, bf16x8_t row) { both[j % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row, k[j / 2], both[j % 2], 0, 0, 0); });
+            const bool ragged = key0 + kKeys > lowest || __builtin_amdgcn_readfirstlane(out);       // not every row adds something and sees all of the keys
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const f32x16_t& x = both[half];
@@ -370,7 +384,6 @@ __device__ __forceinline__ void weigh_tiles(const WeighArgs& a, int s, int kh, i
     }
     float w = sum[0] + sum[1] + (sum[2] + sum[3]);
     w += __shfl_xor(w, 32);
-    if (none) w = __builtin_nanf("");
     if (h != 0) return;
     const int64_t weights = ((int64_t)s * a.cache.kv_heads + kh) * a.w_stride;
     put_weight(a, q, weights, key0 + col, w, key0 + col < q.pos0 ? as_global(a.w)[weights + key0 + col] : 0.f);
