@@ -174,6 +174,14 @@ __device__ __forceinline__ bool load_keys(bf16x8_t (&k)[D / 16], const WeighArgs
     return page >= 0;
 }
 
+// In front of it a wavefront's lanes have written to LDS what its others read behind it, or read what the others write: the wavefront's operations there stay in
+// this order by themselves, the compiler, for which a lane is a thread of its own, has to be told.
+__device__ __forceinline__ void lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Many rows and few keys: a workgroup has 32 keys, and its wavefronts take the rows 32 at a time in turn, straight from memory; their sums meet in LDS.
 constexpr int wide_waves(int head_dim) { return head_dim == 256 ? 8 : 16; }       // as many as have registers for it
 
@@ -210,10 +218,12 @@ __device__ __forceinline__ void weigh_wide(const WeighArgs& a, int s, int kh, in
     if (first < rows) ask((int)first);
     for (int r = (int)first; r < rows; r += kStep) {
         const int sees = lse == kNone ? 0 : limit;               // 0 also for rows that are not there
+        lanes_meet();
         if (h == 0) {                                            // (of this wavefront's own)
             sh_lse[wave][col] = lse * kLog2e;
             sh_limit[wave][col] = sees;
         }
+        lanes_meet();
         const bool ragged = __any(key0 + 32 > sees);
         f32x16_t x;
 #pragma unroll
