@@ -561,7 +561,8 @@ typedef struct {
  * 2^125; a cell is the value over the power rounded to the nearest, ties to even codes, and six where it is beyond six.  32 values one
  * of which is a NaN or infinite become NaN.  Where two tokens of a batch have the same place, what is there is of neither (codes of the
  * one may meet powers of the other).
- *   k->out, v->out  bf16 rows for what the new tokens' cells stand for (exact in bf16), or NULL; rows without a place become zeros
+ *   k->out, v->out  bf16 rows for what the new tokens' cells stand for (exact in bf16), or NULL; rows without a place become zeros.  As
+ *                   q->out they may be x (bf16, the same strides)
  *   positions       DEVICE, n_tokens: where the rotation takes a token to be, for caches that tokens were evicted from; one outside
  *                   0 .. n_pos - 1 turns by NaN.  NULL: its position in the cache.
  * Errors as patch_kv_append. */
@@ -586,8 +587,8 @@ typedef struct {
  * before it (W is not read there).  For sequences with tokens in the call and j < kv_len[s]; everything else stays as it is.
  *   Q, q_stride, heads  as in patch_attention, whose lse (n_tokens x heads) for these rows is `lse`
  *   W, W_out            DEVICE, n_seqs x kv_heads rows of `stride` >= max_kv floats, 16-byte aligned, stride a multiple of 4; W_out may be W
- * A row whose lse is minus infinity (it saw nothing) adds nothing, whatever its query and the keys are.  Sums are fp32, in an order that the sizes alone decide.  Pages that are
- * not followed have NaN for keys.  Errors: PATCH_ERR_ARG, PATCH_ERR_SHAPE, PATCH_ERR_HIP. */
+ * A row whose lse is minus infinity (it saw nothing) adds nothing, whatever its query and the keys are.  Sums are fp32, in an order that
+ * the sizes alone decide.  Pages that are not followed have NaN for keys.  Errors: PATCH_ERR_ARG, PATCH_ERR_SHAPE, PATCH_ERR_HIP. */
 patch_status patch_attention_weights(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache* cache, const float* lse,
                                      const float* W, float* W_out, int64_t stride, void* stream, const patch_weights_opts* opts);
 patch_status patch_attention_weights4(const void* Q, int64_t q_stride, int heads, const patch_seqs* seqs, const patch_kv_cache4* cache, const float* lse,

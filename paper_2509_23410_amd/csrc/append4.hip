@@ -5,6 +5,10 @@
 //
 // A head is D / 8 threads with eight features each, so that 32 features are four neighbours and a thread's cells are one word of K.  Where halves of a head are
 // rotated against each other a thread loads its features' partners too (they are in the cache, another thread has them as its own) and turns only its own.
+//
+// Rows may be written where they are read (out is x).  A head's threads are in one wavefront, and each stores what it computed from all of their loads.  A tile of V reads
+// rows of its own positions only; what it reads for a position that is not new may have been written already, and goes nowhere.  Rows without a place, which the threads of K's
+// heads clear, are in no tile.
 #include "cells4.h"
 
 namespace patch {
