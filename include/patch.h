@@ -608,8 +608,10 @@ typedef struct {
 /* Each key head of each sequence keeps `keep` of its tokens: those that always stay, then those of the largest weight W (a NaN is the
  * smallest); of equal ones, and of those that always stay if there are more than `keep`, those in lower slots.  Tokens in slots below
  * `keep` that stay do so where they are; the others, in the order of their slots, move into the slots there that became free, in
- * theirs.  So keys are in no order afterwards and differ from head to head: new tokens are appended behind them as always, with
- * positions given for their rotation.
+ * theirs.  So keys are in no order afterwards and differ from head to head.  New tokens are appended behind them, rotated by their
+ * positions in the text, which are not their slots: patch_kv_append4 is told those.  patch_kv_append is not and turns by the slot, so for
+ * bf16 and e4m3 cells patch_qk_rope turns Q and K first, into rows of their own, and the append has them (q: NULL) with rope = NULL; K
+ * then is rounded to bf16 before it is to e4m3.
  *   seqs   n_seqs (times kv_heads at most 2^21), kv_len, page_table, table_stride and max_kv; n_tokens, q_start and max_q are not looked at
  *   W      DEVICE, n_seqs x kv_heads rows of `stride` >= max_kv floats, 16-byte aligned, stride a multiple of 4
  * Pages that two sequences share may only be in front of their sinks.  Cells whose page, or whose goal's, is not followed stay; a

@@ -727,7 +727,8 @@ def patch_kv_evict(seqs: Seqs, cache: KVCache, W, W_out, stride: int, keep: int,
                    positions=None, positions_out=None) -> None:
     """Each key head of each sequence keeps `keep` tokens: the first `sinks`, the last `recent`, and those of the largest weight W (n_seqs x kv_heads rows of
     `stride` floats).  Those behind slot `keep` move into the slots that became free; W_out and positions_out (may be W and positions, or None) follow.
-    moved_from (device int32, n_seqs x kv_heads x keep): the slot that each slot's token came from; kv_len_out: tokens afterwards."""
+    moved_from (device int32, n_seqs x kv_heads x keep): the slot that each slot's token came from; kv_len_out: tokens afterwards.
+    A token that is appended later has another position than its slot: patch_qk_rope before patch_kv_append without a rope; patch_kv_append4 takes positions."""
     _evict(lib().patch_kv_evict, "patch_kv_evict", seqs, cache, W, W_out, stride, keep, moved_from, kv_len_out, stream, sinks, recent, positions, positions_out)
 
 
