@@ -614,8 +614,10 @@ typedef struct {
  * then is rounded to bf16 before it is to e4m3.
  *   seqs   n_seqs (times kv_heads at most 2^21), kv_len, page_table, table_stride and max_kv; n_tokens, q_start and max_q are not looked at
  *   W      DEVICE, n_seqs x kv_heads rows of `stride` >= max_kv floats, 16-byte aligned, stride a multiple of 4
- * Pages that two sequences share may only be in front of their sinks.  Cells whose page, or whose goal's, is not followed stay; a
- * sequence longer than max_kv or the table stays as it is (`from` is -1).  Errors: PATCH_ERR_ARG, PATCH_ERR_SHAPE, PATCH_ERR_HIP. */
+ * Every token in a page that sequences share has to be one that always stays, in a slot below `keep`: the moves of one sequence would
+ * change what the others have.  So sinks are at least the shared front, and behind one longer than `keep` nothing can be evicted.  Cells
+ * whose page, or whose goal's, is not followed stay; a sequence longer than max_kv or the table stays as it is (`from` is -1).
+ * Errors: PATCH_ERR_ARG, PATCH_ERR_SHAPE, PATCH_ERR_HIP. */
 patch_status patch_kv_evict(const patch_seqs* seqs, const patch_kv_cache* cache, const float* W, int64_t stride, const patch_evict_opts* opts, void* stream);
 patch_status patch_kv_evict4(const patch_seqs* seqs, const patch_kv_cache4* cache, const float* W, int64_t stride, const patch_evict_opts* opts, void* stream);
 
