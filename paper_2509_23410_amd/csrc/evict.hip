@@ -130,15 +130,18 @@ struct Ranks {
 // Histograms are four side by side, of every fourth lane each: an atomic add takes as long as its most frequent address has lanes.
 constexpr int kCopies = 4, kBins = 2048;
 
-// Slots whose tokens stay are a bit each where a head has more than registers hold; of so many at most (and ranks near the border in as many pairs of the ring).
-constexpr int kMaskWords = 6656, kNear = 8192;
+// Slots whose tokens stay are a bit each where a head has more than registers hold; of so many at most.  Those near the border (between the kMargin-th of the sample in
+// front of it and the kMargin-th behind, see near_border) are a list of ranks and slots.  It holds as many as the longest of these heads is expected to have there and
+// five standard deviations more (sqrt(2 kMargin) of the sample's): with 8192 the list ran out from 200000 slots on, and 205000, half of which stay, took 276 us for 140.
+constexpr int kMaskWords = 6656, kMargin = 320, kNear = 10240;
+static_assert(kNear >= 32 * kMaskWords / 16384 * (2 * kMargin + 5 * 26), "the list and the bits are for heads of the same length");
 
 template <int J, int RING, int MASK>
 struct SelectLds {
     int count[kBins * kCopies];
     uint32_t strip[J][kWaves];         // counts of a strip's wavefronts
     int wave[kWaves], found[3];
-    int movers[RING];                  // slots behind the budget whose tokens stay
+    int movers[MASK > 1 && RING < 2 * kNear ? 2 * kNear : RING];      // a ring of slots behind the budget whose tokens stay, or the list of those near the border
     uint32_t mask[MASK];
 };
 
@@ -321,7 +324,7 @@ struct Block {
 template <int J, typename Lds, typename Stream>
 __device__ __forceinline__ bool near_border(Ranks<J>& ranks, Lds& sh, int keep, int len, const float* w, const int32_t* pos, const Always& always, const Stream& stream) {
     static_assert(J * kStrip == 16384, "a sample");
-    constexpr int kMargin = 320;                                 // five standard deviations of how many of 16384 are above the border, where that is the median
+    // (kMargin is five standard deviations of how many of 16384 are above the border, where that is the median)
     const int tid = threadIdx.x, lane = tid & 63;
     if (len > 32 * kMaskWords) return false;
     ranks.sample(w, pos, len, always);
