@@ -97,7 +97,7 @@ size_t plan_attention(AttnArgs* a, size_t ws_bytes) {
         int64_t own_blocks = resident;
         if (a->prefix) {
             // What both cost in workgroups' time where all share the memory, in us: 64 keys for 128 rows of the front 3, 128 keys of a sequence 7, in e4m3 half of
-            // that.  Taken at heads of 128 in bf16 and used for the other sizes too, as a ratio.  The longest sequence is all that the host knows, and the
+            // that.  Taken at heads of 128 in bf16 and used for the other sizes too, as a ratio, and e4m3's for 4-bit cells.  The longest sequence is all that the host knows, and the
             // others are taken to be half as long on the whole: right within a factor of two or so where max_kv is close to the lengths, and if it is far
             // beyond them the front has too few workgroups (64 sequences of up to 9000 tokens, 8192 shared, the same inputs each time: 47 us, and 238 with max_kv = 65536).
             const double f = 3.0 * front_units * over(a->prefix, 64), o = (a->cache.cells == kBf16 ? 7.0 : 3.5) * 0.5 * notes * over(std::max<int64_t>(own, 1), 128);

@@ -635,7 +635,8 @@ struct TilesLds {
 // product(j, operand(j)) for j = 0 .. N - 1, in this order and with five operands asked for ahead: left to itself the compiler asks for one at a time, and waits.
 // Both products of the tiles so, against the order asked for with sched_group_barrier in the first and none in the second: 6 pieces of up to 700 tokens over
 // 8 key heads of 4 151 us before and 138 so in bf16, 165 and 141 in e4m3, 167 and 146 in e2m1; a prompt of 4096 over 32 heads of 128 in bf16 165 and 156.
-// Six ahead take the same time but spill at 128 features.
+// Six ahead take the same time but spill at 128 features.  Five cost a kernel of heads of 64 its third wavefront on a SIMD (179 registers for 159) and the few-row kernel of
+// 128 beside a shared front two spilled registers, and no time: 32 pieces of 30 tokens over 8 heads of 64 76.6 us before and 73.8, 64 sequences behind 8192 44.8 and 42.8.
 template <int N, typename Operand, typename Product>
 __device__ __forceinline__ void in_order(const Operand& operand, const Product& product) {
     constexpr int kLead = N < 5 ? N : 5;
@@ -656,7 +657,7 @@ template <int D, int NW, int CELLS>
 __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const Span& p, int kh, int half, int first_row, TilesLds<D, NW>& sh) {
     constexpr int kTile = TilesLds<D, NW>::kTile, kBlocks = kTile / 32;        // keys at a time, as 32 to an instruction
     constexpr int DV = TilesLds<D, NW>::DV;
-    constexpr int kThreads = 64 * NW, kLoad = CELLS == kE2m1 && NW == 8 ? 8 : 16;                  // bytes of a load: every thread has one
+    constexpr int kThreads = 64 * NW, kLoad = CELLS == kE2m1 && NW == 8 ? 8 : 16;                  // bytes of a load; a small tile has fewer loads than there are threads
     constexpr int kCells = CELLS == kE2m1 ? 2 * kLoad : CELLS == kE4m3 ? 16 : 8;
     constexpr int kRows = CELLS == kE2m1 ? 2 : 1, kRunKeys = kCells / kRows;   // a load of V: so many features of so many keys
     typedef typename std::conditional<kLoad == 8, u32x2_t, u32x4_t>::type Load;

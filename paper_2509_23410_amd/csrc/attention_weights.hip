@@ -56,8 +56,8 @@ struct KeyTile {
 };
 
 // Few rows (16 RB at most): each wavefront has `steps` steps of 64 keys, straight from memory into the operands' registers, the next step's on their way.  Memory
-// bounds it: 32 sequences of up to 8000 tokens, 8 key heads of 128 in 4 bits, 27.6 us, 3.7 TB/s (a large copy: 5.0); with a step's page numbers looked up when it is
-// asked for 38.
+// bounds it: 32 sequences of up to 8000 tokens, 8 key heads of 128 in 4 bits, 26.3 us, 3.9 TB/s (a large copy: 5.0); with a step's page numbers looked up when it is
+// asked for 38, with branches around the loads of lse 27.6.
 template <int D, int RB, int CELLS>
 __global__ __launch_bounds__(256, 2) void weigh_few_kernel(const WeighArgs a, const int steps) {
     const int s = blockIdx.y, kh = blockIdx.x % a.cache.kv_heads, lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
